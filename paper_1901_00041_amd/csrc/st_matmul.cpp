@@ -1,0 +1,357 @@
+// Matrix products of several tenants: validation, choice of tiles, work lists and the C ABI (include/st_lm.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "st_host.h"
+#include "st_lm_host.h"
+#include "st_lm_internal.h"
+
+using namespace st;
+
+struct st_matmul {
+  std::vector<st_matmul_desc> descs;
+  std::vector<st_matmul_tenant_info> info;
+  std::vector<MatmulDev> tenants;      // host mirror of the device table
+  struct Launch { int dtype, shape; int64_t begin, count; };
+  std::vector<Launch> launches;
+  std::vector<MatmulItem> items;       // of all launches, one after another
+  st_matmul_plan_info totals = {};
+  int device = 0;
+  char* d_arena = nullptr;             // the one device allocation: table, items, counters, partial tiles
+  MatmulDev* d_tenants = nullptr;
+  MatmulItem* d_items = nullptr;
+};
+
+namespace {
+
+constexpr uint32_t kActs = ST_EPI_RELU | ST_EPI_GELU | ST_EPI_GELU_TANH | ST_EPI_SILU;
+constexpr uint32_t kResiduals = ST_EPI_RESIDUAL | ST_EPI_RESIDUAL_LAST;
+
+int64_t row_of(int64_t ld, int64_t dense) { return ld ? ld : dense; }
+
+// What a matrix of rows spans; whether two of them share a byte.
+struct Span {
+  uintptr_t at;
+  int64_t rows, row_bytes, turn;     // turn: bytes from a row to the next
+  uintptr_t end() const { return at + (uintptr_t)((rows - 1) * turn + row_bytes); }
+};
+bool overlap(const Span& a, const Span& b) {
+  if (a.rows <= 0 || b.rows <= 0 || a.at >= b.end() || b.at >= a.end()) return false;
+  if (a.turn == b.turn) {             // columns of one matrix that lie beside each other
+    const int64_t off = (((int64_t)b.at - (int64_t)a.at) % a.turn + a.turn) % a.turn;      // where b's rows start in a's
+    if (off >= a.row_bytes && off + b.row_bytes <= a.turn) return false;
+  }
+  return true;
+}
+
+st_status validate_sizes(const st_matmul_desc& d, int t) {
+  if (d.M < 0 || d.N <= 0 || d.K <= 0) return fail(ST_ERR_INVALID_ARG, "tenant %d: N and K must be positive and M not negative", t);
+  if (d.in_dtype != ST_DT_F32 && d.in_dtype != ST_DT_BF16 && d.in_dtype != ST_DT_F16)
+    return fail(ST_ERR_UNSUPPORTED, "tenant %d: unknown in_dtype %d", t, d.in_dtype);
+  if (d.out_dtype != ST_DT_F32 && d.out_dtype != d.in_dtype)
+    return fail(ST_ERR_UNSUPPORTED, "tenant %d: out_dtype must be f32 or equal to in_dtype", t);
+  if (d.epilogue & ~(kActs | kResiduals | ST_EPI_BIAS)) return fail(ST_ERR_UNSUPPORTED, "tenant %d: unknown epilogue bits 0x%x", t, d.epilogue);
+  if (__builtin_popcount(d.epilogue & kActs) > 1) return fail(ST_ERR_INVALID_ARG, "tenant %d: more than one activation", t);
+  if ((d.epilogue & kResiduals) == kResiduals) return fail(ST_ERR_INVALID_ARG, "tenant %d: the residual is added once, before or after the activation", t);
+  const bool res = (d.epilogue & kResiduals) != 0;
+  if (d.ldx < 0 || d.ldw < 0 || d.ldy < 0 || d.ldr < 0 || (d.ldx && d.ldx < d.K) || (d.ldw && d.ldw < d.K) || (d.ldy && d.ldy < d.N) || (res && d.ldr && d.ldr < d.N))
+    return fail(ST_ERR_INVALID_ARG, "tenant %d: rows must not overlap the rows behind them", t);
+  if (d.K > kMatmulMaxK || d.N > kMatmulMaxK || std::max(std::max(d.ldx, d.ldw), std::max(d.ldy, res ? d.ldr : 0)) > kMatmulMaxLd)
+    return fail(ST_ERR_UNSUPPORTED, "tenant %d: rows of at most %d elements, at most %d apart", t, kMatmulMaxK, kMatmulMaxLd);
+  return ST_OK;
+}
+
+st_status validate_pointers(const st_matmul_desc& d, const st_matmul_desc& p, int t) {      // sizes from d, pointers from p
+  if (d.M == 0) return ST_OK;
+  const bool res = (d.epilogue & kResiduals) != 0, bias = (d.epilogue & ST_EPI_BIAS) != 0;
+  if (!p.x || !p.w || !p.y) return fail(ST_ERR_INVALID_ARG, "tenant %d: x, w and y must be non-NULL", t);
+  if (bias && !p.bias) return fail(ST_ERR_INVALID_ARG, "tenant %d: ST_EPI_BIAS without a bias pointer", t);
+  if (res && !p.residual) return fail(ST_ERR_INVALID_ARG, "tenant %d: a residual bit without a residual pointer", t);
+  const int64_t es = elem_size(d.in_dtype), os = elem_size(d.out_dtype);
+  if ((uintptr_t)p.x % es || (uintptr_t)p.w % es || (bias && (uintptr_t)p.bias % es) || (uintptr_t)p.y % os || (res && (uintptr_t)p.residual % os))
+    return fail(ST_ERR_INVALID_ARG, "tenant %d: a pointer is not a multiple of its element's size", t);
+  const Span y = {(uintptr_t)p.y, d.M, d.N * os, row_of(d.ldy, d.N) * os};
+  const Span x = {(uintptr_t)p.x, d.M, d.K * es, row_of(d.ldx, d.K) * es}, w = {(uintptr_t)p.w, d.N, d.K * es, row_of(d.ldw, d.K) * es};
+  if (overlap(y, x) || overlap(y, w) || (bias && overlap(y, Span{(uintptr_t)p.bias, 1, d.N * es, d.N * es})))
+    return fail(ST_ERR_INVALID_ARG, "tenant %d: y must not overlap x, w or bias", t);
+  const int64_t ldr = row_of(d.ldr, d.N);
+  if (res && !(p.residual == p.y && ldr == row_of(d.ldy, d.N)) && overlap(y, Span{(uintptr_t)p.residual, d.M, d.N * os, ldr * os}))
+    return fail(ST_ERR_INVALID_ARG, "tenant %d: residual must be y itself or not overlap it", t);
+  return ST_OK;
+}
+
+void set_pointers(MatmulDev& T, const st_matmul_desc& d, const st_matmul_desc& p) {
+  T.x = p.x; T.w = p.w; T.y = p.y;
+  T.bias = (d.epilogue & ST_EPI_BIAS) ? p.bias : nullptr;
+  T.res = (d.epilogue & kResiduals) ? p.residual : nullptr;
+  const int64_t os = elem_size(d.out_dtype);
+  auto aligned = [](const void* q, int64_t ld_bytes) { return (uintptr_t)q % 16 == 0 && ld_bytes % 16 == 0; };
+  T.vec = (aligned(T.y, T.ldy * os) ? kMatmulVecY : 0u) | (aligned(T.res, T.ldr * os) ? kMatmulVecRes : 0u) | (aligned(T.bias, 0) ? kMatmulVecBias : 0u);
+}
+
+// ---- choice of a tile shape and of a division of the reduction -----------------------------------------------------------
+struct Choice { int shape, split, per_split; double clocks; };
+
+int steps_of(const st_matmul_desc& d, int shape) {
+  const int bytes = kMatmulShapes[shape].skinny ? kMatmulUnitBytes : kMatmulStepBytes;
+  return cdiv((int64_t)(d.K / (16 / elem_size(d.in_dtype))) * 16, bytes);
+}
+
+// Clocks until a tenant is done that has `share` of the chip to itself.
+double clocks_of(const st_matmul_desc& d, int shape, int split, double share) {
+  const MatmulShape& S = kMatmulShapes[shape];
+  const int steps = steps_of(d, shape), per = std::max(1, cdiv(steps, split)), es = elem_size(d.in_dtype);
+  const int64_t items = (int64_t)cdiv(d.M, S.MT) * cdiv(d.N, S.NT) * split;
+  double item, resident;
+  if (S.skinny) {
+    const int in_flight = 2 * (S.MT / 16 + S.NT / 16 <= 2 ? 8 : S.MT / 16 + S.NT / 16 <= 4 ? 4 : 2);
+    resident = 2;
+    const double unit = std::max(2000.0 / in_flight, (S.MT + S.NT) * 64 * 4.0 * resident / 40.0 / 4.0);
+    item = 2500 + cdiv(per, 4) * unit;
+  } else {
+    const double mfma = (double)S.MT * S.NT * (kMatmulStepBytes / es) * 2 / (es == 4 ? 256 : 4096) / 0.75, load = (S.MT + S.NT) * 128 / 40.0;
+    resident = shape == 0 ? 1 : 2;
+    item = 3500 + S.MT * S.NT / 12.0 + per * std::max(resident * std::max(mfma, load), shape == 2 ? 450.0 : 900.0);
+  }
+  if (split > 1) item += 2000 + split * S.MT * S.NT * 4 / 64.0;
+  const double rounds = std::max(1.0, std::ceil(items / (kNumCUs * resident * share) - 1e-9));
+  return std::max(rounds * item, ((double)d.N * d.K + (double)d.M * d.K) * es / (2200 * share));
+}
+
+Choice choose(const st_matmul_desc& d, double share, const st_plan_opts& o) {
+  Choice best = {-1, 1, 1, 0};
+  for (int shape = 0; shape < kNumMatmulShapes; ++shape) {
+    const MatmulShape& S = kMatmulShapes[shape];
+    if (o.tile_cfg ? o.tile_cfg - 1 != shape : (S.skinny && (d.M > S.MT || (d.M <= S.MT / 2 && S.MT > 16)))) continue;
+    const int steps = steps_of(d, shape);
+    for (int want = 1; want <= 32; ++want) {
+      if (o.split_k && want != 1) break;
+      int split = std::max(1, std::min(o.split_k ? o.split_k : want, steps));
+      const int per = std::max(1, cdiv(steps, split));
+      split = std::max(1, cdiv(steps, per));
+      const Choice c = {shape, split, per, clocks_of(d, shape, split, share)};
+      if (best.shape < 0 || c.clocks < best.clocks) best = c;
+    }
+  }
+  return best;
+}
+
+// A tenant's items: blocks of 4 x 8 tiles, so that the workgroups that run side by side on an XCD share rows of x and w in its L2, cut
+// into one stretch per XCD (workgroup b of a launch runs on XCD b mod 8).
+void deal(int t, const st_matmul_tenant_info& ti, std::vector<MatmulItem> (&xcd)[kNumXCDs], int start) {
+  std::vector<MatmulItem> all;
+  all.reserve((size_t)ti.item_count);
+  for (int bn = 0; bn < ti.tiles_n; bn += 8)
+    for (int bm = 0; bm < ti.tiles_m; bm += 4)
+      for (int n = bn; n < std::min(bn + 8, ti.tiles_n); ++n)
+        for (int m = bm; m < std::min(bm + 4, ti.tiles_m); ++m)
+          for (int s = 0; s < ti.split_k; ++s) all.push_back({(uint32_t)t, (uint32_t)m, (uint32_t)n, (uint32_t)s});
+  const int64_t n = (int64_t)all.size();
+  for (int x = 0; x < kNumXCDs; ++x)
+    for (int64_t i = n * x / kNumXCDs; i < n * (x + 1) / kNumXCDs; ++i) xcd[(x + start) % kNumXCDs].push_back(all[(size_t)i]);
+}
+
+st_status upload(st_matmul* p) {
+  const size_t n = p->tenants.size();
+  auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
+  size_t ws = 0, counters = 0;
+  for (size_t t = 0; t < n; ++t) {
+    const st_matmul_tenant_info& ti = p->info[t];
+    if (ti.split_k > 1) {
+      ws += (size_t)ti.tiles_m * ti.tiles_n * ti.split_k * ti.MT * ti.NT * 4;
+      counters += (size_t)ti.tiles_m * ti.tiles_n;
+    }
+  }
+  p->totals.workspace_bytes = (int64_t)(ws + counters * 4);
+  if (p->totals.host_only || p->items.empty()) return ST_OK;
+  const size_t off_items = up(n * sizeof(MatmulDev)), off_counters = off_items + up(p->items.size() * sizeof(MatmulItem)), off_ws = off_counters + up(counters * 4);
+  ST_HIP(hipGetDevice(&p->device));
+  ST_HIP(hipMalloc((void**)&p->d_arena, off_ws + ws));
+  p->d_tenants = (MatmulDev*)p->d_arena;
+  p->d_items = (MatmulItem*)(p->d_arena + off_items);
+  size_t wf = off_ws, ct = off_counters;
+  for (size_t t = 0; t < n; ++t) {
+    const st_matmul_tenant_info& ti = p->info[t];
+    if (ti.split_k <= 1) continue;
+    p->tenants[t].ws = (float*)(p->d_arena + wf);
+    p->tenants[t].counters = (uint32_t*)(p->d_arena + ct);
+    wf += (size_t)ti.tiles_m * ti.tiles_n * ti.split_k * ti.MT * ti.NT * 4;
+    ct += (size_t)ti.tiles_m * ti.tiles_n * 4;
+  }
+  std::vector<char> host(off_ws, 0);
+  std::memcpy(host.data(), p->tenants.data(), n * sizeof(MatmulDev));
+  std::memcpy(host.data() + off_items, p->items.data(), p->items.size() * sizeof(MatmulItem));
+  ST_HIP(hipMemcpy(p->d_arena, host.data(), off_ws, hipMemcpyHostToDevice));
+  return ST_OK;
+}
+
+st_status build(st_matmul* p, const st_matmul_desc* descs, int n, const st_plan_opts& o) {
+  p->descs.assign(descs, descs + n);
+  p->info.assign((size_t)n, st_matmul_tenant_info{});
+  p->tenants.assign((size_t)n, MatmulDev{});
+  p->totals.n_tenants = n;
+  p->totals.host_only = o.host_only;
+  std::vector<double> work((size_t)n, 0.0), clocks((size_t)n, 0.0);
+  double all = 0;
+  for (int t = 0; t < n; ++t) {
+    const st_matmul_desc& d = descs[t];
+    const int64_t es = elem_size(d.in_dtype), os = elem_size(d.out_dtype);
+    if (d.M == 0) continue;
+    const double flops = 2.0 * d.M * d.N * d.K;
+    const int64_t bytes = ((int64_t)d.M * d.K + (int64_t)d.N * d.K + ((d.epilogue & ST_EPI_BIAS) ? d.N : 0)) * es + (int64_t)d.M * d.N * os * ((d.epilogue & kResiduals) ? 2 : 1);
+    p->totals.flops += 2 * (int64_t)d.M * d.N * d.K;
+    p->totals.bytes += bytes;
+    work[t] = std::max(flops / (es == 4 ? 256 : 4096) / kNumCUs, bytes / 2200.0);
+    all += work[t];
+  }
+  for (int t = 0; t < n; ++t) {
+    const st_matmul_desc& d = descs[t];
+    st_matmul_tenant_info& ti = p->info[t];
+    MatmulDev& T = p->tenants[t];
+    T.M = d.M; T.N = d.N; T.K = d.K;
+    T.ldx = (int32_t)row_of(d.ldx, d.K); T.ldw = (int32_t)row_of(d.ldw, d.K); T.ldy = (int32_t)row_of(d.ldy, d.N); T.ldr = (int32_t)row_of(d.ldr, d.N);
+    T.epilogue = d.epilogue;
+    T.out_f32 = d.out_dtype == ST_DT_F32;
+    set_pointers(T, d, d);
+    const Choice c = choose(d, all > 0 ? std::max(work[t] / all, 1.0 / 4096) : 1.0, o);
+    const MatmulShape& S = kMatmulShapes[c.shape];
+    ti.tile_cfg = c.shape;
+    ti.MT = S.MT; ti.NT = S.NT;
+    ti.tiles_m = cdiv(d.M, S.MT); ti.tiles_n = cdiv(d.N, S.NT);
+    ti.split_k = d.M ? c.split : 1;
+    if ((double)ti.tiles_m * ti.tiles_n * ti.split_k >= 2147483648.0) return fail(ST_ERR_UNSUPPORTED, "tenant %d: more than 2^31 work items", t);
+    ti.item_count = (int64_t)ti.tiles_m * ti.tiles_n * ti.split_k;
+    T.tiles_n = ti.tiles_n; T.split = ti.split_k; T.per_split = c.per_split;
+    clocks[t] = c.clocks;
+    p->totals.n_items += ti.item_count;
+  }
+  if (p->totals.n_items >= ((int64_t)1 << 31)) return fail(ST_ERR_UNSUPPORTED, "more than 2^31 work items");
+  for (int dtype = 0; dtype < 3; ++dtype)
+    for (int shape = 0; shape < kNumMatmulShapes; ++shape) {
+      std::vector<int> mine;
+      for (int t = 0; t < n; ++t)
+        if (p->info[t].item_count && descs[t].in_dtype == dtype && p->info[t].tile_cfg == shape) mine.push_back(t);
+      if (mine.empty()) continue;
+      // tenants whose items take longest come first
+      std::stable_sort(mine.begin(), mine.end(), [&](int a, int b) { return p->tenants[a].per_split > p->tenants[b].per_split; });
+      std::vector<MatmulItem> xcd[kNumXCDs];
+      int start = 0;
+      for (int t : mine) {
+        deal(t, p->info[t], xcd, start);
+        start = (int)((start + p->info[t].item_count) % kNumXCDs);
+      }
+      const int64_t begin = (int64_t)p->items.size();
+      size_t most = 0;
+      for (const auto& l : xcd) most = std::max(most, l.size());
+      for (size_t i = 0; i < most; ++i)
+        for (const auto& l : xcd)
+          if (i < l.size()) p->items.push_back(l[i]);
+      p->launches.push_back({dtype, shape, begin, (int64_t)p->items.size() - begin});
+    }
+  p->totals.launches = (int32_t)p->launches.size();
+  return upload(p);
+}
+
+}  // namespace
+
+extern "C" st_status st_matmul_plan(const st_matmul_desc* descs, int32_t n_tenants, const st_plan_opts* opts, st_matmul** out_plan) {
+  if (!out_plan) return fail(ST_ERR_INVALID_ARG, "out_plan is NULL");
+  *out_plan = nullptr;
+  if (n_tenants < 0 || (n_tenants > 0 && !descs)) return fail(ST_ERR_INVALID_ARG, "descs is NULL or n_tenants negative");
+  st_plan_opts o;
+  std::memset(&o, 0, sizeof(o));
+  if (opts) o = *opts;
+  if (o.tile_cfg < 0 || o.tile_cfg > kNumMatmulShapes || o.split_k < 0 || o.reserved != 0) return fail(ST_ERR_INVALID_ARG, "bad plan options");
+  for (int t = 0; t < n_tenants; ++t) {
+    st_status s = validate_sizes(descs[t], t);
+    if (s == ST_OK) s = validate_pointers(descs[t], descs[t], t);
+    if (s != ST_OK) return s;
+  }
+  st_matmul* p = new (std::nothrow) st_matmul();
+  if (!p) return fail(ST_ERR_OUT_OF_MEMORY, "host allocation failed");
+  st_status s;
+  try {
+    s = build(p, descs, n_tenants, o);
+  } catch (const std::exception&) {
+    s = fail(ST_ERR_OUT_OF_MEMORY, "host allocation failed");
+  }
+  if (s != ST_OK) {
+    st_matmul_destroy(p);
+    return s;
+  }
+  *out_plan = p;
+  return ST_OK;
+}
+
+extern "C" st_status st_matmul_run(const st_matmul* plan, void* hip_stream) {
+  if (!plan) return fail(ST_ERR_INVALID_ARG, "plan is NULL");
+  if (plan->totals.host_only) return fail(ST_ERR_UNSUPPORTED, "plan was built host-only and cannot run");
+  if (plan->launches.empty()) return ST_OK;
+  OnDevice on(plan->device);
+  ST_HIP(on.error);
+  for (const st_matmul::Launch& l : plan->launches)
+    ST_HIP((hipError_t)launch_matmul(l.dtype, l.shape, plan->d_tenants, plan->d_items + l.begin, l.count, hip_stream));
+  return ST_OK;
+}
+
+extern "C" st_status st_matmul_rebind_all(st_matmul* plan, const st_matmul_desc* descs, int32_t n_tenants, void* hip_stream) {
+  if (!plan) return fail(ST_ERR_INVALID_ARG, "plan is NULL");
+  if (n_tenants != (int32_t)plan->tenants.size()) return fail(ST_ERR_INVALID_ARG, "n_tenants differs from the plan's");
+  if (n_tenants > 0 && !descs) return fail(ST_ERR_INVALID_ARG, "descs is NULL");
+  for (int t = 0; t < n_tenants; ++t) {
+    const st_status s = validate_pointers(plan->descs[t], descs[t], t);
+    if (s != ST_OK) return s;
+  }
+  std::vector<MatmulDev> next;
+  try {
+    next = plan->tenants;
+  } catch (const std::exception&) {
+    return fail(ST_ERR_OUT_OF_MEMORY, "host allocation failed");
+  }
+  for (int t = 0; t < n_tenants; ++t) set_pointers(next[t], plan->descs[t], descs[t]);
+  if (n_tenants == 0 || std::memcmp(next.data(), plan->tenants.data(), next.size() * sizeof(MatmulDev)) == 0) return ST_OK;
+  if (!plan->totals.host_only && plan->d_tenants) {
+    OnDevice on(plan->device);
+    ST_HIP(on.error);
+    ST_HIP((hipError_t)launch_poke(next.data(), (int64_t)(next.size() * sizeof(MatmulDev)), plan->d_tenants, hip_stream));
+  }
+  plan->tenants.swap(next);
+  for (int t = 0; t < n_tenants; ++t) {
+    st_matmul_desc& d = plan->descs[t];
+    d.x = descs[t].x; d.w = descs[t].w; d.bias = descs[t].bias; d.y = descs[t].y; d.residual = descs[t].residual;
+  }
+  return ST_OK;
+}
+
+extern "C" st_status st_matmul_get_info(const st_matmul* plan, st_matmul_plan_info* out) {
+  if (!plan || !out) return fail(ST_ERR_INVALID_ARG, "NULL argument");
+  *out = plan->totals;
+  return ST_OK;
+}
+
+extern "C" st_status st_matmul_get_tenant_info(const st_matmul* plan, int32_t tenant, st_matmul_tenant_info* out) {
+  if (!plan || !out) return fail(ST_ERR_INVALID_ARG, "NULL argument");
+  if (tenant < 0 || (size_t)tenant >= plan->info.size()) return fail(ST_ERR_INVALID_ARG, "tenant index out of range");
+  *out = plan->info[(size_t)tenant];
+  return ST_OK;
+}
+
+extern "C" void st_matmul_destroy(st_matmul* plan) {
+  if (!plan) return;
+  if (plan->d_arena) (void)hipFree(plan->d_arena);
+  delete plan;
+}
+
+extern "C" st_status st_matmul_tile_shape(int32_t index, int32_t* MT, int32_t* NT) {
+  if (!MT || !NT) return fail(ST_ERR_INVALID_ARG, "NULL argument");
+  if (index < 0 || index >= kNumMatmulShapes) return fail(ST_ERR_INVALID_ARG, "tile index out of range");
+  *MT = kMatmulShapes[index].MT;
+  *NT = kMatmulShapes[index].NT;
+  return ST_OK;
+}
+extern "C" int32_t st_matmul_tile_count(void) { return kNumMatmulShapes; }

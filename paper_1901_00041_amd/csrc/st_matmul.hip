@@ -1,0 +1,488 @@
+// Matrix products of several tenants for gfx950 (MI355X): y = act(x w^T + bias + residual), one workgroup per output tile or slice
+// of its reduction.
+//
+// Both operands have the reduction index contiguous, so a 16-byte chunk of a row is an MFMA operand as it stands.  w is operand A
+// and x operand B: a lane then ends with 4 consecutive outputs of one row.  The reduction runs over whole 16-byte chunks; what is
+// left of a row (K off the vector) is one more MFMA step whose operands are put together element by element.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "st_launch.h"
+#include "st_lm_internal.h"
+#include "st_tiles.hpp"
+
+namespace st {
+
+typedef __attribute__((address_space(4))) const MatmulDev ConstMatmul;
+typedef __attribute__((address_space(4))) const MatmulItem ConstMatmulItem;
+
+// ---- epilogue -------------------------------------------------------------------------------------------------------
+// erfc(z) e^(z^2) for z >= 0 as a polynomial in t = 1 / (1 + z/2), fitted to relative error 2^-23 over [0, 10]; with it
+// v/2 erfc(-v/sqrt 2) keeps its relative accuracy in both tails, where 1 + erf would cancel.
+__device__ __forceinline__ float gelu_f32(float v) {
+  return 0.5f * v * erfcf(v * -0.70710678118654752f);
+}
+__device__ __forceinline__ float exp_neg(float v) { return __builtin_amdgcn_exp2f(v * -1.4426950408889634f); }      // e^-v
+__device__ __forceinline__ float silu_f32(float v) { return v * __builtin_amdgcn_rcpf(1.f + exp_neg(v)); }
+// v/2 (1 + tanh u) = v / (1 + e^(-2u))
+__device__ __forceinline__ float gelu_tanh_f32(float v) {
+  const float u = 1.5957691216057308f * (v + 0.044715f * v * v * v);
+  return v * __builtin_amdgcn_rcpf(1.f + exp_neg(u));
+}
+
+__device__ __forceinline__ float load_elem(const void* p, int64_t i, bool f32, int dt) {
+  if (f32) return ((const float*)p)[i];
+  const uint16_t h = ((const uint16_t*)p)[i];
+  return dt == ST_DT_BF16 ? bf16_bits_to_f32(h) : f16_bits_to_f32(h);
+}
+
+template <int W>
+__device__ __forceinline__ void activate(uint32_t epi, float (&v)[W]) {
+  if (epi & ST_EPI_RELU) {
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = relu_f32(v[e]);
+  } else if (epi & ST_EPI_GELU) {
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = gelu_f32(v[e]);
+  } else if (epi & ST_EPI_GELU_TANH) {
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = gelu_tanh_f32(v[e]);
+  } else if (epi & ST_EPI_SILU) {
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = silu_f32(v[e]);
+  }
+}
+
+// W (4 or 8) consecutive values of one row, from 16-byte (or, four 16-bit ones, 8-byte) aligned memory
+template <int DT, int W>
+__device__ __forceinline__ void load_row(const void* p, int64_t i, bool f32, float (&v)[W]) {
+  if (DT == ST_DT_F32 || f32) {
+#pragma unroll
+    for (int q = 0; q < W / 4; ++q) {
+      const f32x4 a = *(const f32x4*)((const float*)p + i + 4 * q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * q + e] = a[e];
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < W / 4; ++q) {
+      const uint2 a = *(const uint2*)((const uint16_t*)p + i + 4 * q);
+      v[4 * q] = unpack16<DT>(a.x, 0);
+      v[4 * q + 1] = unpack16<DT>(a.x, 1);
+      v[4 * q + 2] = unpack16<DT>(a.y, 0);
+      v[4 * q + 3] = unpack16<DT>(a.y, 1);
+    }
+  }
+}
+
+// W consecutive outputs [n, n + W) of row m from their sums
+template <int DT, int W>
+__device__ __forceinline__ void finish_row(ConstMatmul& T, int64_t m, int n, float (&v)[W]) {
+  const uint32_t epi = T.epilogue, vec = T.vec;
+  const int left = T.N - n;
+  if (left <= 0) return;
+  const bool whole = left >= W, f32 = DT == ST_DT_F32 || T.out_f32 != 0;
+  if (epi & ST_EPI_BIAS) {
+    float b[W];
+    if (whole && (vec & kMatmulVecBias)) {
+      load_row<DT, W>(T.bias, n, false, b);
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; ++e) b[e] = e < left ? load_elem(T.bias, n + e, DT == ST_DT_F32, DT) : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] += b[e];
+  }
+  float r[W];
+  if (epi & (ST_EPI_RESIDUAL | ST_EPI_RESIDUAL_LAST)) {
+    const int64_t at = m * T.ldr + n;
+    if (whole && (vec & kMatmulVecRes)) {
+      load_row<DT, W>(T.res, at, f32, r);
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; ++e) r[e] = e < left ? load_elem(T.res, at + e, f32, DT) : 0.f;
+    }
+  }
+  if (epi & ST_EPI_RESIDUAL) {
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] += r[e];
+  }
+  activate(epi, v);
+  if (epi & ST_EPI_RESIDUAL_LAST) {
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] += r[e];
+  }
+  const int64_t at = m * T.ldy + n;
+  if (f32) {
+    float* y = (float*)T.y + at;
+    if (whole && (vec & kMatmulVecY)) {
+#pragma unroll
+      for (int q = 0; q < W / 4; ++q) *(f32x4*)(y + 4 * q) = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; ++e)
+        if (e < left) y[e] = v[e];
+    }
+  } else if constexpr (DT != ST_DT_F32) {
+    uint16_t* y = (uint16_t*)T.y + at;
+    uint32_t o[W / 2];
+#pragma unroll
+    for (int e = 0; e < W / 2; ++e) o[e] = pack16<DT>(v[2 * e], v[2 * e + 1]);
+    if (whole && (vec & kMatmulVecY)) {
+      if constexpr (W == 8) *(u32x4*)y = u32x4{o[0], o[1], o[2], o[3]};
+      else *(uint2*)y = make_uint2(o[0], o[1]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; ++e)
+        if (e < left) y[e] = (uint16_t)(o[e / 2] >> (16 * (e & 1)));
+    }
+  }
+}
+
+// The elements of a row behind its whole 16-byte chunks, as one chunk; zeros for a row that there is not.
+template <int DT>
+__device__ __forceinline__ u32x4 row_end(const void* p, int64_t row, int64_t rows, int ld, int K, bool mine) {
+  constexpr int ES = ElemOf<DT>::ES, VEC = 16 / ES;
+  const int whole = K / VEC * VEC;
+  u32x4 out = {0u, 0u, 0u, 0u};
+  if (!mine || row >= rows) return out;
+#pragma unroll
+  for (int e = 0; e < VEC - 1; ++e) {
+    if (whole + e < K) {
+      const int64_t i = row * ld + whole + e;
+      if constexpr (ES == 4) out[e] = ((const uint32_t*)p)[i];
+      else out[e >> 1] |= (uint32_t)((const uint16_t*)p)[i] << (16 * (e & 1));
+    }
+  }
+  return out;
+}
+
+// Publishes this workgroup's partial sums and returns whether it is the last of its tile, which then has the slices' sum, in slice
+// order.  get(q) / set(q, v): the thread's q-th group of four sums.  As in st_tiles.hpp: device-scope stores and loads, no L2-wide
+// fence, nobody waits.
+template <int NQ, int THREADS, class Get, class Set>
+__device__ __forceinline__ bool join_slices(ConstMatmul& T, const MatmulItem it, Get&& get, Set&& set, uint32_t* flag) {
+  const int tid = (int)threadIdx.x, split = T.split;
+  const int64_t tile = (int64_t)it.tile_m * T.tiles_n + it.tile_n;
+  constexpr uint32_t kSlice = NQ * THREADS * 16;
+  float* base = T.ws + tile * split * (kSlice / 4);
+  const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, (uint32_t)split * kSlice);
+  static_for<NQ>([&](auto Q) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, get(Q)), rs, (decltype(Q)::value * THREADS + tid) * 16, (int)(it.slice * kSlice), kAuxDeviceCoherent);
+  });
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (tid == 0) {
+    const uint32_t old = __hip_atomic_fetch_add(&T.counters[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const uint32_t last = old == (uint32_t)(split - 1);
+    if (last) __hip_atomic_store(&T.counters[tile], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last;
+  }
+  __syncthreads();
+  if (*flag == 0u) return false;
+  constexpr int QB = NQ < 4 ? NQ : 4, SB = 4;
+  static_assert(NQ % QB == 0, "batches");
+  static_for<NQ / QB>([&](auto Q0) {
+    constexpr int q0 = decltype(Q0)::value * QB;
+    f32x4 sum[QB];
+#pragma unroll
+    for (int q = 0; q < QB; ++q) sum[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < split; s0 += SB) {
+      f32x4 part[SB][QB];
+#pragma unroll
+      for (int s = 0; s < SB; ++s)
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+          const uint32_t off = s0 + s < split ? (uint32_t)(((q0 + q) * THREADS + tid) * 16) : kInvalidOffset;
+          part[s][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, (s0 + s) * (int)kSlice, kAuxDeviceCoherent));
+        }
+#pragma unroll
+      for (int s = 0; s < SB; ++s)
+#pragma unroll
+        for (int q = 0; q < QB; ++q) sum[q] += part[s][q];
+    }
+    static_for<QB>([&](auto Q) { set(std::integral_constant<int, q0 + decltype(Q)::value>{}, sum[decltype(Q)::value]); });
+  });
+  return true;
+}
+
+// ---- few rows: the weights stream from memory to registers -----------------------------------------------------------
+// 16 R rows x 16 F outputs per workgroup.  The four wavefronts divide the slice's reduction; a lane (i = lane mod 16, g = lane / 16)
+// loads 16 bytes of output row i and of row i of x, chunk g of a 64-byte unit, which is a 16x16 MFMA operand; the four partial
+// sums meet in LDS.  Bound by reading w once; x is small and comes from the L2 for every workgroup.
+template <int DT, int R, int F>
+__global__ __launch_bounds__(256) void st_matmul_skinny_kernel(const MatmulDev* table, const MatmulItem* items) {
+  constexpr int ES = ElemOf<DT>::ES, VEC = 16 / ES;
+  constexpr int UN = R + F <= 2 ? 8 : R + F <= 4 ? 4 : 2;      // units in flight, twice over
+  __shared__ f32x4 part[4][R * F][64];
+  __shared__ uint32_t flag;
+  const ConstMatmulItem& ci = ((ConstMatmulItem*)items)[blockIdx.x];
+  const MatmulItem it = {ci.tenant, ci.tile_m, ci.tile_n, ci.slice};
+  ConstMatmul& T = ((ConstMatmul*)table)[it.tenant];
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
+  const int m0 = (int)it.tile_m * 16 * R, n0 = (int)it.tile_n * 16 * F;
+  const int rows_x = T.M - m0 < 16 * R ? T.M - m0 : 16 * R, rows_w = T.N - n0 < 16 * F ? T.N - n0 : 16 * F;
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc((const char*)T.x + (int64_t)m0 * T.ldx * ES, (uint32_t)(((int64_t)(rows_x - 1) * T.ldx + T.K) * ES));
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc((const char*)T.w + (int64_t)n0 * T.ldw * ES, (uint32_t)(((int64_t)(rows_w - 1) * T.ldw + T.K) * ES));
+  const int chunks = T.K / VEC, units = (chunks + 3) / 4;
+  const int s_begin = (int)it.slice * T.per_split, s_end = s_begin + T.per_split < units ? s_begin + T.per_split : units;
+  const int each = (s_end - s_begin + 3) / 4;
+  int u = s_begin + wave * each;
+  const int u_end = u + each < s_end ? u + each : s_end;
+
+  uint32_t ox[R], ow[F];
+#pragma unroll
+  for (int r = 0; r < R; ++r) ox[r] = r * 16 + i < rows_x ? (uint32_t)((r * 16 + i) * T.ldx * ES + g * 16) : kInvalidOffset;
+#pragma unroll
+  for (int f = 0; f < F; ++f) ow[f] = f * 16 + i < rows_w ? (uint32_t)((f * 16 + i) * T.ldw * ES + g * 16) : kInvalidOffset;
+  typedef Mma<DT, 16> Op;
+  f32x4 acc[F][R];
+#pragma unroll
+  for (int f = 0; f < F; ++f)
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  struct Batch { u32x4 x[UN][R], w[UN][F]; };
+  auto fetch = [&](Batch& b, int at) {
+#pragma unroll
+    for (int s = 0; s < UN; ++s) {
+      // a unit past the range, or a chunk past the row, is out of every buffer's range
+      const uint32_t kill = (at + s < u_end && (at + s) * 4 + g < chunks) ? 0u : kInvalidOffset;
+#pragma unroll
+      for (int f = 0; f < F; ++f) b.w[s][f] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)((ow[f] + (uint32_t)((at + s) * 64)) | kill), 0, 0);
+#pragma unroll
+      for (int r = 0; r < R; ++r) b.x[s][r] = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)((ox[r] + (uint32_t)((at + s) * 64)) | kill), 0, 0);
+    }
+  };
+  auto multiply = [&](const Batch& b) {
+#pragma unroll
+    for (int s = 0; s < UN; ++s)
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[f][r] = Op::run(b.w[s][f], b.x[s][r], acc[f][r]);
+  };
+  if (u < u_end) {
+    Batch b0, b1;
+    fetch(b0, u);
+    for (; u < u_end; u += 2 * UN) {
+      fetch(b1, u + UN);
+      multiply(b0);
+      fetch(b0, u + 2 * UN);
+      multiply(b1);
+    }
+  }
+  if (T.K % VEC != 0 && s_end == units && wave == 3) {
+    u32x4 ex[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) ex[r] = row_end<DT>(T.x, (int64_t)m0 + r * 16 + i, T.M, T.ldx, T.K, g == 0);
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      const u32x4 ew = row_end<DT>(T.w, (int64_t)n0 + f * 16 + i, T.N, T.ldw, T.K, g == 0);
+#pragma unroll
+      for (int r = 0; r < R; ++r) acc[f][r] = Op::run(ew, ex[r], acc[f][r]);
+    }
+  }
+#pragma unroll
+  for (int f = 0; f < F; ++f)
+#pragma unroll
+    for (int r = 0; r < R; ++r) part[wave][f * R + r][lane] = acc[f][r];
+  __syncthreads();
+  // a thread takes four outputs of a row: block q, lane l of the MFMA layout
+  constexpr int NQ = (R * F + 3) / 4;
+  f32x4 v[NQ];
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) {
+    const int q = k * 4 + wave;
+    v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (q < R * F) v[k] = (part[0][q][lane] + part[1][q][lane]) + (part[2][q][lane] + part[3][q][lane]);
+  }
+  if (T.split > 1 && !join_slices<NQ, 256>(T, it, [&](auto Q) { return v[decltype(Q)::value]; }, [&](auto Q, f32x4 s) { v[decltype(Q)::value] = s; }, &flag)) return;
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) {
+    const int q = k * 4 + wave;
+    if (q < R * F) {
+      const int f = q / R, r = q % R, m = m0 + r * 16 + i;
+      float o[4] = {v[k][0], v[k][1], v[k][2], v[k][3]};
+      if (m < T.M) finish_row<DT, 4>(T, m, n0 + f * 16 + 4 * g, o);
+    }
+  }
+}
+
+// ---- tiles through LDS -------------------------------------------------------------------------------------------------
+// MT rows x NT outputs, WM x WN wavefronts, 32x32 MFMA blocks, 128 bytes of the reduction per row and step, ST steps resident.
+// Operands go from memory to LDS directly, 16-byte chunk c of row r to position c ^ (r mod 8), so that the eight rows that an
+// operand read takes at a time lie in different banks.  One barrier per step, placed before the last quarter of its MFMAs: by then
+// all its operands are in registers, so its stage can be refilled and the next step's operands read while that quarter runs.
+template <int DT, int MT, int NT, int WM, int WN, int ST>
+__global__ __launch_bounds__(WM * WN * 64) void st_matmul_tile_kernel(const MatmulDev* table, const MatmulItem* items) {
+  constexpr int ES = ElemOf<DT>::ES, VEC = 16 / ES, KB = kMatmulStepBytes, WAVES = WM * WN, THREADS = WAVES * 64;
+  constexpr int BM = MT / WM / 32, BN = NT / WN / 32;
+  constexpr int kStage = (MT + NT) * KB, LX = MT * KB / 1024 / WAVES, LW = NT * KB / 1024 / WAVES, NL = LX + LW;
+  constexpr int NW = BN * 32, kPitch = NW + 4;                  // epilogue: floats per row in LDS
+  constexpr int kOut = WAVES * 32 * kPitch * 4;
+  constexpr int kSmem = ST * kStage > kOut ? ST * kStage : kOut;
+  static_assert(LX * WAVES * 1024 == MT * KB && LW * WAVES * 1024 == NT * KB, "whole load instructions");
+  __shared__ __align__(128) char smem[kSmem];
+  __shared__ uint32_t flag;
+  const ConstMatmulItem& ci = ((ConstMatmulItem*)items)[blockIdx.x];
+  const MatmulItem it = {ci.tenant, ci.tile_m, ci.tile_n, ci.slice};
+  ConstMatmul& T = ((ConstMatmul*)table)[it.tenant];
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm0 = (wave % WM) * BM * 32, wn0 = (wave / WM) * BN * 32;
+  const int m0 = (int)it.tile_m * MT, n0 = (int)it.tile_n * NT;
+  const int rows_x = T.M - m0 < MT ? T.M - m0 : MT, rows_w = T.N - n0 < NT ? T.N - n0 : NT;
+  const u32x4 rx = rsrc_words((const char*)T.x + (int64_t)m0 * T.ldx * ES, (uint32_t)(((int64_t)(rows_x - 1) * T.ldx + T.K) * ES));
+  const u32x4 rw = rsrc_words((const char*)T.w + (int64_t)n0 * T.ldw * ES, (uint32_t)(((int64_t)(rows_w - 1) * T.ldw + T.K) * ES));
+  const int chunks = T.K / VEC, steps = (chunks + 7) / 8;
+  const int s_begin = (int)it.slice * T.per_split, s_end = s_begin + T.per_split < steps ? s_begin + T.per_split : steps;
+
+  const int lrow = lane >> 3, chunk = (lane & 7) ^ lrow;
+  uint32_t vx[LX], vw[LW];
+#pragma unroll
+  for (int l = 0; l < LX; ++l) {
+    const int row = (l * WAVES + wave) * 8 + lrow;
+    vx[l] = row < rows_x ? (uint32_t)(row * T.ldx * ES + chunk * 16) : kInvalidOffset;
+  }
+#pragma unroll
+  for (int l = 0; l < LW; ++l) {
+    const int row = (l * WAVES + wave) * 8 + lrow;
+    vw[l] = row < rows_w ? (uint32_t)(row * T.ldw * ES + chunk * 16) : kInvalidOffset;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + (uint32_t)wave * 1024u;
+  // load instruction L of step s, into the stage at LDS offset `stage`; past the range and past the row's end every lane is out of range
+  auto issue = [&](auto L, int s, uint32_t stage, uint32_t kill) {
+    constexpr int l = decltype(L)::value;
+    const uint32_t soff = (uint32_t)s * KB;
+    if constexpr (l < LX) load_to_lds<0, l * WAVES * 1024>(rx, vx[l] | kill, soff, lds0 + stage);
+    else load_to_lds<0, MT * KB + (l - LX) * WAVES * 1024>(rw, vw[l - LX] | kill, soff, lds0 + stage);
+  };
+  auto killed = [&](int s) { return s < s_end && s * 8 + chunk < chunks ? 0u : kInvalidOffset; };
+
+  typedef Mma<DT, 32> Op;
+  typename Op::Acc acc[BN][BM];
+#pragma unroll
+  for (int j = 0; j < BN; ++j)
+#pragma unroll
+    for (int i = 0; i < BM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[j][i][e] = 0.f;
+
+  struct Frags { u32x4 x[BM], w[BN]; };
+  const int r32 = lane & 31, half = lane >> 5;
+  uint32_t sub_off[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) sub_off[s] = (uint32_t)(r32 * KB + (((s * 2 + half) ^ (r32 & 7)) << 4));
+  auto read = [&](Frags& f, uint32_t stage, int sub) {
+#pragma unroll
+    for (int j = 0; j < BN; ++j) f.w[j] = *(const u32x4*)(smem + stage + sub_off[sub] + MT * KB + (wn0 + j * 32) * KB);
+#pragma unroll
+    for (int i = 0; i < BM; ++i) f.x[i] = *(const u32x4*)(smem + stage + sub_off[sub] + (wm0 + i * 32) * KB);
+  };
+  auto multiply = [&](const Frags& f) {
+#pragma unroll
+    for (int j = 0; j < BN; ++j)
+#pragma unroll
+      for (int i = 0; i < BM; ++i) acc[j][i] = Op::run(f.w[j], f.x[i], acc[j][i]);
+  };
+
+  if (s_begin < s_end) {
+#pragma unroll
+    for (int s = 0; s < ST; ++s) {
+      const uint32_t kill = killed(s_begin + s);
+      static_for<NL>([&](auto L) { issue(L, s_begin + s, s * kStage, kill); });
+    }
+    wait_loads_barrier<(ST - 1) * NL>();
+    Frags f0, f1;
+    read(f0, 0, 0);
+    uint32_t cur = 0;
+    for (int s = s_begin; s < s_end; ++s) {
+      const uint32_t next = cur + kStage < ST * kStage ? cur + kStage : 0;
+      const uint32_t kill = killed(s + ST);
+      read(f1, cur, 1);
+      multiply(f0);
+      read(f0, cur, 2);
+      multiply(f1);
+      read(f1, cur, 3);
+      multiply(f0);
+      wait_loads_barrier<(ST - 2) * NL>();
+      static_for<NL>([&](auto L) { issue(L, s + ST, cur, kill); });
+      read(f0, next, 0);
+      multiply(f1);
+      cur = next;
+    }
+  }
+  if (T.K % VEC != 0 && s_end == steps) {
+    Frags f;
+#pragma unroll
+    for (int j = 0; j < BN; ++j) f.w[j] = row_end<DT>(T.w, (int64_t)n0 + wn0 + j * 32 + r32, T.N, T.ldw, T.K, half == 0);
+#pragma unroll
+    for (int i = 0; i < BM; ++i) f.x[i] = row_end<DT>(T.x, (int64_t)m0 + wm0 + i * 32 + r32, T.M, T.ldx, T.K, half == 0);
+    multiply(f);
+  }
+  wait_loads_barrier<0>();          // nothing is on its way into LDS any more, and nobody reads operands
+
+  if (T.split > 1) {
+    auto get = [&](auto Q) {
+      constexpr int q = decltype(Q)::value, j = q / 4 / BM, i = q / 4 % BM, g = q % 4;
+      return f32x4{acc[j][i][4 * g], acc[j][i][4 * g + 1], acc[j][i][4 * g + 2], acc[j][i][4 * g + 3]};
+    };
+    auto set = [&](auto Q, f32x4 v) {
+      constexpr int q = decltype(Q)::value, j = q / 4 / BM, i = q / 4 % BM, g = q % 4;
+      acc[j][i][4 * g] = v[0], acc[j][i][4 * g + 1] = v[1], acc[j][i][4 * g + 2] = v[2], acc[j][i][4 * g + 3] = v[3];
+    };
+    if (!join_slices<BN * BM * 4, THREADS>(T, it, get, set, &flag)) return;
+  }
+  // A wavefront turns its rows round in LDS of its own, 32 of them at a time, so that a row's outputs leave together.
+  float* mine = (float*)smem + wave * 32 * kPitch;
+  constexpr int LPR = NW / 8, RPP = 64 / LPR;
+  const int c8 = lane % LPR * 8, rr = lane / LPR;
+  static_for<BM>([&](auto I) {
+    constexpr int i = decltype(I)::value;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < BN; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(f32x4*)(mine + r32 * kPitch + j * 32 + 8 * g + 4 * half) = f32x4{acc[j][i][4 * g], acc[j][i][4 * g + 1], acc[j][i][4 * g + 2], acc[j][i][4 * g + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int p = 0; p < 32 / RPP; ++p) {
+      const int r = p * RPP + rr;
+      const int64_t m = (int64_t)m0 + wm0 + i * 32 + r;
+      float o[8];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const f32x4 a = *(const f32x4*)(mine + r * kPitch + c8 + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[4 * q + e] = a[e];
+      }
+      if (m < T.M) finish_row<DT, 8>(T, m, n0 + wn0 + c8, o);
+    }
+  });
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------------
+template <int DT>
+static hipError_t launch_shape(int shape, unsigned blocks, void* stream, const MatmulDev* table, const MatmulItem* items) {
+  switch (shape) {
+    case 0: return launch(st_matmul_tile_kernel<DT, 256, 256, 4, 2, 2>, blocks, 512, stream, table, items);
+    case 1: return launch(st_matmul_tile_kernel<DT, 128, 128, 2, 2, 2>, blocks, 256, stream, table, items);
+    case 2: return launch(st_matmul_tile_kernel<DT, 64, 64, 2, 2, 4>, blocks, 256, stream, table, items);
+    case 3: return launch(st_matmul_skinny_kernel<DT, 4, 2>, blocks, 256, stream, table, items);
+    case 4: return launch(st_matmul_skinny_kernel<DT, 2, 2>, blocks, 256, stream, table, items);
+    case 5: return launch(st_matmul_skinny_kernel<DT, 1, 2>, blocks, 256, stream, table, items);
+    case 6: return launch(st_matmul_skinny_kernel<DT, 1, 1>, blocks, 256, stream, table, items);
+  }
+  return hipErrorInvalidValue;
+}
+
+int launch_matmul(int dtype, int shape, const MatmulDev* table_dev, const MatmulItem* items_dev, int64_t n_items, void* stream) {
+  if (n_items <= 0) return 0;
+  const auto run = dtype == ST_DT_F32 ? launch_shape<ST_DT_F32> : dtype == ST_DT_BF16 ? launch_shape<ST_DT_BF16> : launch_shape<ST_DT_F16>;
+  return (int)run(shape, (unsigned)n_items, stream, table_dev, items_dev);
+}
+
+}  // namespace st

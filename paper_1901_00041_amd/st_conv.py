@@ -26,7 +26,10 @@ EXPORTS = ["st_conv_plan", "st_conv_run", "st_conv_run_noalloc", "st_conv_noallo
            "st_plan_cache_create", "st_plan_cache_get", "st_plan_cache_get_stats", "st_plan_cache_destroy", "st_conv_plan_info", "st_conv_plan_tenant_info", "st_conv_plan_tenant_form", "st_conv_plan_worklist",
            "st_conv_plan_destroy", "st_chain_plan", "st_chain_run", "st_chain_run_profiled", "st_chain_aborted", "st_chain_set_wait_limit_us",
            "st_chain_get_info", "st_chain_get_op_info", "st_chain_worklist", "st_chain_columns", "st_chain_dependencies", "st_chain_set_workgroups", "st_chain_destroy", "st_tile_shape", "st_tile_count", "st_maxpool_nhwc",
-           "st_launch_empty", "st_launch_copy", "st_status_string", "st_last_error_message"]
+           "st_launch_empty", "st_launch_copy", "st_status_string", "st_last_error_message",
+           # include/st_lm.h (bound in st_lm.py)
+           "st_matmul_plan", "st_matmul_run", "st_matmul_rebind_all", "st_matmul_get_info", "st_matmul_get_tenant_info", "st_matmul_destroy",
+           "st_matmul_tile_shape", "st_matmul_tile_count"]
 
 
 class st_conv_desc(ctypes.Structure):

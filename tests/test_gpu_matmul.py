@@ -1,0 +1,288 @@
+"""Products of several tenants (st_matmul_*) through the C ABI against the formula in 64 bits.
+
+Tolerance of an output, element by element, with e = 2^-24 (half a step of fp32): a sum of K products in fp32 is off by at most
+2 e (K + 4) sum|x w| (a matrix instruction may round each addition by a whole step); bias and residual add a rounding each; an activation passes the error on with a slope of
+at most 1.13 and adds its own, relative to its value: the exponential's argument a is rounded, so e^a is off by |a| e times a few
+steps, the rest by a few; at last half a step of the output's type."""
+import itertools
+import math
+
+import pytest
+
+from paper_1901_00041_amd import st_conv as sc
+from paper_1901_00041_amd import st_lm
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+ACTS = {"none": 0, "relu": st_lm.ST_EPI_RELU, "gelu": st_lm.ST_EPI_GELU, "gelu_tanh": st_lm.ST_EPI_GELU_TANH, "silu": st_lm.ST_EPI_SILU}
+
+
+def torch_():
+    import torch
+    return torch
+
+
+def dt(name):
+    torch = torch_()
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+class Product:
+    """One tenant: rows `pad` elements further apart than they are long, `shift` elements behind an aligned address, NaN around them."""
+
+    def __init__(self, m, n, k, dtype, out, act="none", bias=False, residual="none", pad=0, shift=0, seed=0, gain=1.0, in_place=False):
+        torch = torch_()
+        gen = torch.Generator().manual_seed(seed * 1000003 + m * 10007 + n * 101 + k)
+        self.m, self.n, self.k, self.dtype, self.out, self.act, self.residual = m, n, k, dtype, out, act, residual
+
+        def rows(r, c, t, scale=1.0):
+            whole = torch.full((r * (c + pad) + shift,), float("nan"), dtype=dt(t))
+            view = whole[shift:].view(r, c + pad)[:, :c]
+            view.copy_(torch.randn(r, c, generator=gen) * scale)
+            whole = whole.cuda()
+            return whole, whole[shift:].view(r, c + pad)[:, :c]
+
+        self.keep = []
+        self.x, self.w, self.bias, self.res = None, None, None, None
+        whole, self.x = rows(m, k, dtype, gain)
+        self.keep.append(whole)
+        whole, self.w = rows(n, k, dtype, k ** -0.5)
+        self.keep.append(whole)
+        if bias:
+            whole, b = rows(1, n, dtype)
+            self.bias = b[0]
+            self.keep.append(whole)
+        self.whole_y, self.y = rows(m, n, out)
+        if residual != "none":
+            if in_place:
+                self.res = self.y
+            else:
+                whole, self.res = rows(m, n, out)
+                self.keep.append(whole)
+        self.reference()
+        if not in_place:
+            self.whole_y.fill_(float("nan"))
+        self.ld = (k + pad, k + pad, n + pad, n + pad)
+
+    def desc(self):
+        bits = ACTS[self.act] | (st_lm.ST_EPI_BIAS if self.bias is not None else 0)
+        bits |= {"none": 0, "before": st_lm.ST_EPI_RESIDUAL, "last": st_lm.ST_EPI_RESIDUAL_LAST}[self.residual]
+        return st_lm.make_matmul_desc(self.m, self.n, self.k, self.dtype, self.out, self.x, self.w, self.y, bias=self.bias, residual=self.res, epilogue=bits,
+                                      ldx=self.ld[0], ldw=self.ld[1], ldy=self.ld[2], ldr=self.ld[3])
+
+    def reference(self):
+        torch = torch_()
+        x, w = self.x.double().cpu(), self.w.double().cpu()
+        v = x @ w.t()
+        off = 2 * E * (self.k + 4) * (x.abs() @ w.abs().t())
+        if self.bias is not None:
+            v = v + self.bias.double().cpu()
+            off = off + E * v.abs()
+        r = self.res.double().cpu() if self.res is not None else 0.0
+        if self.residual == "before":
+            v = v + r
+            off = off + E * v.abs()
+        if self.act == "relu":
+            v = torch.where(v > 0, v, torch.zeros_like(v))
+        elif self.act == "gelu":
+            g = 0.5 * v * torch.erfc(v / -math.sqrt(2.0))
+            off, v = 1.13 * off + E * (8 * v * v + 32) * g.abs(), g
+        elif self.act == "gelu_tanh":
+            u = math.sqrt(8 / math.pi) * (v + 0.044715 * v ** 3)
+            g = v * torch.sigmoid(u)
+            off, v = 1.13 * off + E * (8 * u.abs() + 32) * g.abs(), g
+        elif self.act == "silu":
+            g = v * torch.sigmoid(v)
+            off, v = 1.1 * off + E * (8 * v.abs() + 32) * g.abs(), g
+        if self.residual == "last":
+            v = v + r
+            off = off + E * v.abs()
+        self.want = v
+        eps = {"f32": 2.0 ** -23, "bf16": 2.0 ** -7, "f16": 2.0 ** -10}[self.out]        # torch.finfo(t).eps: bf16 2^-7, fp16 2^-10
+        tiny = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -24}[self.out]
+        self.tol = off + (v.abs() + off) * eps / 2 + tiny
+
+    def check(self, what=""):
+        torch = torch_()
+        got = self.y.double().cpu()
+        assert torch.isfinite(got).all(), f"{what}: not written, or not finite"
+        over = (got - self.want).abs() / self.tol
+        assert over.max() <= 1.0, f"{what}: {over.max():.2f} tolerances off at {divmod(int(over.argmax()), self.n)}"
+        gap = self.whole_y.clone()
+        shift = gap.numel() - self.m * self.ld[2]
+        gap[shift:].view(self.m, self.ld[2])[:, :self.n] = float("nan")
+        assert torch.isnan(gap).all(), f"{what}: wrote outside its rows"
+
+
+def run(products, stream=None, **opts):
+    torch = torch_()
+    plan = st_lm.st_matmul_plan([p.desc() for p in products], sc.plan_opts(**opts) if opts else None, keep=products)
+    torch.cuda.synchronize()
+    st_lm.st_matmul_run(plan, stream)
+    torch.cuda.synchronize()
+    return plan
+
+
+SIZES = [(1, 1, 1), (1, 16, 64), (3, 17, 33), (16, 32, 128), (5, 130, 1000), (17, 40, 257), (33, 64, 512), (64, 31, 96), (65, 100, 65), (130, 259, 200), (257, 300, 136)]
+
+
+@pytest.mark.parametrize("dtype, out", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_sizes(size, dtype, out):
+    p = Product(*size, dtype, out, act="relu", bias=True)
+    run([p])
+    p.check()
+
+
+@pytest.mark.parametrize("split", [1, 3])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("cfg", range(7))
+def test_every_tile_shape(cfg, dtype, split):
+    mt, nt = st_lm.st_matmul_tile_shape(cfg)
+    # a whole tile and a bit; one row and one output; K with whole steps, a part of one, elements behind the last vector, and none but these
+    for m, n, k in ((mt + 5, nt + 9, 1024 + 24), (1, 1, 4096), (mt, nt, 643), (mt - 1, 2 * nt, 64), (2, 3, 3), (mt, nt, 130)):
+        p = Product(m, n, k, dtype, "f32" if k % 2 else dtype, act="silu", bias=True, residual="last")
+        plan = run([p], tile_cfg=cfg + 1, split_k=split)
+        p.check(f"{m}x{n}x{k}")
+        p.whole_y.fill_(float("nan"))
+        st_lm.st_matmul_run(plan)              # the counters of a divided reduction are ready for the next run
+        torch_().cuda.synchronize()
+        p.check(f"{m}x{n}x{k} again")
+
+
+@pytest.mark.parametrize("act, bias, residual", [c for c in itertools.product(ACTS, (False, True), ("none", "before", "last")) if c[1] or c[2] != "none" or c[0] != "none"])
+def test_epilogues(act, bias, residual):
+    tenants = [Product(m, 72, 96, d, o, act=act, bias=bias, residual=residual, gain=4.0) for m in (2, 40, 70) for d, o in (("bf16", "bf16"), ("f16", "f32"), ("f32", "f32"))]
+    run(tenants)
+    for i, p in enumerate(tenants):
+        p.check(f"tenant {i}")
+
+
+@pytest.mark.parametrize("pad, shift", [(1, 0), (3, 1), (8, 0), (0, 1), (4, 4), (16, 3)])
+@pytest.mark.parametrize("dtype, out", [("bf16", "bf16"), ("f16", "f32"), ("f32", "f32")])
+def test_rows_anywhere(dtype, out, pad, shift):
+    tenants = [Product(m, n, k, dtype, out, act="gelu", bias=True, residual="before", pad=pad, shift=shift) for m, n, k in ((1, 64, 128), (20, 60, 100), (150, 140, 75))]
+    run(tenants)
+    for i, p in enumerate(tenants):
+        p.check(f"tenant {i}")
+
+
+@pytest.mark.parametrize("residual", ["before", "last"])
+@pytest.mark.parametrize("m", [3, 100])
+def test_added_in_place(m, residual):
+    p = Product(m, 80, 2000, "bf16", "bf16", residual=residual, in_place=True)
+    run([p], split_k=3)
+    p.check()
+
+
+def test_unlike_tenants_in_one_call():
+    tenants = [Product(1, 1024, 1024, "bf16", "bf16", "gelu_tanh", True), Product(33, 50, 70, "f16", "f32"), Product(300, 200, 64, "f32", "f32", "silu"),
+               Product(40, 513, 700, "bf16", "f32", "none", False, "last"), Product(600, 520, 256, "bf16", "bf16", "gelu", True, "before")]
+    empty = st_lm.make_matmul_desc(0, 64, 64, "bf16", "bf16", None, None, None)
+    torch = torch_()
+    plan = st_lm.st_matmul_plan([tenants[0].desc(), empty] + [t.desc() for t in tenants[1:]], keep=tenants)
+    info = st_lm.st_matmul_get_info(plan)
+    assert info.n_tenants == 6 and info.launches >= 3
+    st_lm.st_matmul_run(plan)
+    torch.cuda.synchronize()
+    first = [t.y.clone() for t in tenants]
+    for i, t in enumerate(tenants):
+        t.check(f"tenant {i}")
+        t.whole_y.fill_(float("nan"))
+    st_lm.st_matmul_run(plan)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, t.y) for a, t in zip(first, tenants))
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+def test_values_that_are_not_finite_and_far_ones(act):
+    """Through a product with the identity: every activation at both far ends, at infinity and for NaN."""
+    torch = torch_()
+    values = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 3e38, -3e38, math.inf, -math.inf, math.nan, 88.0, -88.0, 12.0, -12.0, -5.5, 200.0, -200.0, 1e4, -1e4])
+    n = values.numel()
+    bias = values.cuda()
+    x, w = torch.zeros(2, 8, device="cuda"), torch.zeros(n, 8, device="cuda")
+    y = torch.zeros(2, n, device="cuda")
+    plan = st_lm.st_matmul_plan([st_lm.make_matmul_desc(2, n, 8, "f32", "f32", x, w, y, bias=bias, epilogue=ACTS[act] | st_lm.ST_EPI_BIAS)], keep=[x, w, y, bias])
+    st_lm.st_matmul_run(plan)
+    torch.cuda.synchronize()
+    v = values.double()
+    want = {"none": v, "relu": torch.where(v > 0, v, 0.0 * torch.ones_like(v)), "gelu": 0.5 * v * torch.erfc(v / -math.sqrt(2.0)),
+            "gelu_tanh": v / (1.0 + torch.exp(-math.sqrt(8 / math.pi) * (v + 0.044715 * v ** 3))), "silu": v / (1.0 + torch.exp(-v))}[act]
+    # what fp32 makes of these: v * 0 for an infinite v is NaN in the formula of GELU and SiLU, too
+    for row in y.cpu().double():
+        for got, ref, a in zip(row.tolist(), want.tolist(), values.tolist()):
+            if math.isnan(ref) and math.isinf(a):      # the formula's infinity times zero, or its limit
+                assert math.isnan(got) or got == 0.0, (a, got, ref)
+            elif math.isnan(ref):
+                assert math.isnan(got), (a, got, ref)
+            elif math.isinf(ref):
+                assert got == ref, (a, got, ref)
+            else:
+                # a factor below the smallest normal number, 2^-126, may be taken as 0, which is |a| 2^-126 in the value
+                assert abs(got - ref) <= 2e-4 * abs(ref) + (1.0 if math.isnan(a) else abs(a) + 1.0) * 2.0 ** -126, (a, got, ref)
+
+
+def test_a_row_that_is_not_a_number_stays_in_its_row():
+    torch = torch_()
+    for m, n, k, cfg in ((20, 40, 77, 0), (20, 40, 77, 5), (70, 70, 77, 3), (130, 130, 130, 2), (10, 20, 5, 3)):
+        p = Product(m, n, k, "bf16", "f32")
+        want = p.y
+        p.x[3].fill_(float("nan"))
+        p.w[7].fill_(float("inf"))
+        run([p], **({"tile_cfg": cfg} if cfg else {}))
+        got = p.y.cpu()
+        assert torch.isnan(got[3]).all()
+        rest = [r for r in range(m) if r != 3]
+        cols = [c for c in range(n) if c != 7]
+        assert not torch.isfinite(got[rest][:, 7]).any()
+        part = got[rest][:, cols].double()
+        assert torch.isfinite(part).all() and ((part - p.want[rest][:, cols]).abs() <= p.tol[rest][:, cols]).all(), want.shape
+
+
+def test_other_streams_rebinding_and_graphs():
+    torch = torch_()
+    a, b = [[Product(m, 96, 4000, "bf16", "bf16", act="gelu", bias=True, residual="last", seed=s) for m in (1, 90)] for s in (1, 2)]
+    plan = st_lm.st_matmul_plan([p.desc() for p in a], sc.plan_opts(split_k=4), keep=a + b)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    st_lm.st_matmul_run(plan, stream)
+    st_lm.st_matmul_rebind_all(plan, [p.desc() for p in b], stream)
+    st_lm.st_matmul_run(plan, stream)
+    torch.cuda.synchronize()
+    for p in a + b:
+        p.check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st_lm.st_matmul_run(plan, torch.cuda.current_stream())
+    for turn in range(3):
+        for p in b:
+            p.whole_y.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for p in b:
+            p.check(f"replay {turn}")
+            p.whole_y.fill_(float("nan"))
+        st_lm.st_matmul_run(plan)              # eager runs in between
+        torch.cuda.synchronize()
+        for p in b:
+            p.check(f"after replay {turn}")
+
+
+def test_long_rows_and_far_apart_tenants():
+    """Rows 2^21 elements apart: a tile spans 2 GiB, the matrix more."""
+    torch = torch_()
+    m, n, k, ld = 300, 40, 256, 1 << 21
+    whole = torch.empty(m * ld, dtype=torch.float32, device="cuda")
+    x = whole.view(m, ld)[:, :k]
+    x.copy_(torch.randn(m, k, generator=torch.Generator().manual_seed(5)))
+    w = torch.randn(n, k, device="cuda")
+    y = torch.full((m, n), float("nan"), device="cuda")
+    for cfg in (1, 2, 3):
+        y.fill_(float("nan"))
+        plan = st_lm.st_matmul_plan([st_lm.make_matmul_desc(m, n, k, "f32", "f32", x, w, y, ldx=ld)], sc.plan_opts(tile_cfg=cfg), keep=[whole, w, y])
+        st_lm.st_matmul_run(plan)
+        torch.cuda.synchronize()
+        want = x.double() @ w.double().t().contiguous()
+        tol = 2 * E * (k + 4) * (x.double().abs() @ w.double().abs().t().contiguous()) + want.abs() * E
+        assert ((y.double() - want).abs() <= tol).all(), cfg
