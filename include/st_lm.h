@@ -1,10 +1,11 @@
 /*
  * st_lm.h - C ABI of the fused multi-tenant operators of language models for MI355X (gfx950): matrix products with their
- * epilogue.
+ * epilogue, and attention over a paged key-value cache held in 4 bits.
  *
  * They follow st_conv.h (Section 4 of the paper: the kernels of several tenants merged into one launch): an array of
  * per-tenant descriptors with device pointers makes a plan, the plan's run calls issue its work for all tenants together.
- * The conventions of st_conv.h hold:
+ * A decoding step of several tenants is a product (queries, keys and values), st_attn_append, st_attn_run, and the products
+ * that follow, each a call for all of them.  The conventions of st_conv.h hold:
  *   - Tensor pointers are DEVICE pointers, owned by the caller and borrowed by the plan until it is destroyed or rebound.
  *   - Streams are hipStream_t passed as void*; NULL is the default stream.  Run calls are asynchronous, never synchronise and
  *     never allocate device memory, and can be captured into graphs.  A plan belongs to the device that was current when it
@@ -81,6 +82,91 @@ void st_matmul_destroy(st_matmul* plan);
 /* Tile family: rows and outputs of config `index`; ST_ERR_INVALID_ARG past the end. */
 st_status st_matmul_tile_shape(int32_t index, int32_t* MT, int32_t* NT);
 int32_t st_matmul_tile_count(void);
+
+/* ---- Attention over a paged cache in 4 bits -----------------------------------------------------------------------
+ * The cache.  A token's key and value of one head are head_dim elements E2M1 (sign, 2 bits of exponent, 1 of mantissa: 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6) in groups of 32, each with one scale byte s that stands for 2^(s - 127).  Written from values x: with a = max|x| of the
+ * group = m 2^k (1 <= m < 2), the exponent is k - 2 if m <= 1.5 and k - 1 if not, at least -126 and at most 125 (-126 for a = 0), so
+ * that the largest value is never cut off below 2^127; each x is divided by the scale and rounded to the nearest element, ties to the one with the
+ * even code, at most 6.  A value that is not finite makes its token's head unreadable: all its scales become 255 (keys) and 1 (values),
+ * all its codes 0; attention reads its key as not a number and its value as 0.
+ * Attention takes keys and values in the descriptor's dtype, which holds all that is written from that type: bfloat16 any element under a scale of 2^-126 to 2^125, fp16
+ * what it can represent (a scale above 2^13 counts as 2^13, values below 2^-24 are rounded).
+ * A pool is n_pages pages of st_attn_page_bytes() bytes.  A page holds page_tokens tokens: for each key head in turn its
+ * page_tokens / 16 blocks, each of 16 tokens t and head_dim + head_dim / 16 bytes a token:
+ *   keys' codes     [t][head_dim / 2]          byte j holds elements 2j (lower half) and 2j + 1
+ *   values' codes   [16][t][head_dim / 32]     group i of head_dim / 16 elements, two to a byte as above
+ *   keys' scales    [t][head_dim / 32]
+ *   values' scales  [head_dim / 32][t]
+ * A page is one run of bytes that means the same at any index of any pool of the same head layout: copying, forking and moving pages
+ * is copying bytes and writing tables.
+ *
+ * A tenant's sequences.  Sequence i holds length[i] tokens, its new ones included; token p is in page table[i * table_pages +
+ * p / page_tokens].  Its new tokens, the last ones, are rows first[i] .. first[i+1]-1 of q, k, v and out: row first[i] + j is token
+ * p = length[i] - (first[i+1] - first[i]) + j.  table, first and length are read on the device at every run, so that a captured
+ * step can be replayed on other lengths.  Every row that belongs to no sequence is left as it is, in all outputs.
+ *
+ * What a run finds there is checked: a page index outside the pool is not followed (its tokens are not written, and hide from
+ * every query); first is held to [0, max_tokens], what a sequence has more of than max_new new tokens are left out (the rows behind
+ * them are left as they are), and a length is held to [0, table_pages * page_tokens].  st_attn_status reports that it happened. */
+enum { ST_ATTN_CAUSAL = 1u };
+enum { ST_ATTN_BAD_PAGE = 1, ST_ATTN_BAD_LENGTH = 2 };
+
+typedef struct st_attn_desc {
+  int32_t heads, kv_heads;   /* query heads and key heads; heads a multiple of kv_heads: query head h reads key head        */
+                             /* h / (heads / kv_heads)                                                                      */
+  int32_t head_dim;          /* 64, 128 or 256                                                                              */
+  int32_t dtype;             /* ST_DT_BF16 or ST_DT_F16, of q, k, v and the outputs                                          */
+  int32_t n_seqs;            /* sequences, >= 0                                                                             */
+  int32_t max_tokens;        /* rows of q, k, v and the outputs, >= 0                                                       */
+  int32_t max_new;           /* most new tokens of one sequence, >= 1                                                       */
+  int32_t n_pages, page_tokens, table_pages;   /* page_tokens 16, 32, 64, ..., 1024                                         */
+  int32_t window;            /* > 0 (causal only): a token sees itself and the window - 1 tokens before it; 0: all           */
+  uint32_t flags;            /* ST_ATTN_CAUSAL: token p sees tokens 0 .. p of its sequence; else all length[i] of them       */
+  float scale;               /* of the scores, before the softmax; finite                                                   */
+  int32_t reserved;          /* must be 0                                                                                   */
+  int64_t ldq, ldk, ldv, ldo; /* elements from a row to the next of q, k (and k_out), v (and v_out), out; 0 = dense          */
+  const void* q;             /* [max_tokens][heads][head_dim], for st_attn_run                                              */
+  const void *k, *v;         /* [max_tokens][kv_heads][head_dim], for st_attn_append                                        */
+  void* out;                 /* as q, for st_attn_run                                                                       */
+  void *k_out, *v_out;       /* as k and v, for st_attn_read                                                                */
+  void* pages;               /* n_pages * st_attn_page_bytes() bytes, a multiple of 16 as an address                        */
+  const int32_t* table;      /* [n_seqs][table_pages]; entries behind a sequence's last page are not read                   */
+  const int32_t* first;      /* [n_seqs + 1], ascending                                                                     */
+  const int32_t* length;     /* [n_seqs]                                                                                    */
+} st_attn_desc;
+
+typedef struct st_attn_info {
+  int32_t n_tenants, host_only;
+  int32_t launches;          /* kernels of an st_attn_run: tenants of one head_dim, type and kind of division go in one      */
+  int32_t reserved;
+  int64_t n_items;           /* workgroups of these                                                                         */
+  int64_t workspace_bytes;   /* partial results of divided lengths                                                          */
+} st_attn_info;
+
+typedef struct st_attn st_attn; /* opaque */
+
+/* Bytes of a page for these kv_heads, head_dim and page_tokens (nothing else of desc is read); negative if they are not valid. */
+int64_t st_attn_page_bytes(const st_attn_desc* desc);
+/* Validates the descriptors, divides the work by what they allow at most (max_new, table_pages), uploads the tables and allocates the
+ * workspace.  A pointer may be NULL that none of the calls made with the plan needs.  opts: host_only is read, and split_k (> 0:
+ * into how many parts each long sequence's tokens are divided, where they are). */
+st_status st_attn_plan(const st_attn_desc* descs, int32_t n_tenants, const st_plan_opts* opts, st_attn** out_plan);
+/* New tokens' keys and values (k, v) into the cache.  Two sequences that share a page must not both write to it. */
+st_status st_attn_append(const st_attn* plan, void* hip_stream);
+/* What the cache holds of the new tokens, as values of dtype (k_out, v_out).  To read a sequence back from its start, call all of its
+ * tokens new ones.  A token on a page outside the pool reads as 0. */
+st_status st_attn_read(const st_attn* plan, void* hip_stream);
+/* out = softmax(scale q k^T) v over the tokens that each new token sees, which have to be in the cache by now (its own included).
+ * Scores, the softmax's maximum and sum, and the mixed values are held in fp32, weights are rounded to dtype before they
+ * multiply values.  A query that sees no token gets zeros. */
+st_status st_attn_run(const st_attn* plan, void* hip_stream);
+/* All tenants' pointers at once, in stream order: the nine tensors and tables are taken from descs, everything else in them is ignored. */
+st_status st_attn_rebind_all(st_attn* plan, const st_attn_desc* descs, int32_t n_tenants, void* hip_stream);
+/* Waits for the device, then *bits = the ST_ATTN_BAD_* that any run since the last call met; they are cleared. */
+st_status st_attn_status(st_attn* plan, int32_t* bits);
+st_status st_attn_get_info(const st_attn* plan, st_attn_info* out);
+void st_attn_destroy(st_attn* plan);
 
 #ifdef __cplusplus
 }

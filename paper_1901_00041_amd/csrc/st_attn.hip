@@ -1,0 +1,613 @@
+// Attention of several tenants' sequences over paged caches in 4 bits, and the way into and out of these caches, for gfx950 (MI355X).
+//
+// A cache block holds 16 tokens of one head so that MFMA operands come from it without a trip through LDS:
+//   scores   S^T = K Q^T, 16x16 blocks of tokens x query rows.  A lane (i = lane mod 16, g = lane / 16) holds a quarter of token i's
+//            key, dim / 4 elements with one or two scales; which elements meet in one MFMA does not matter as long as the query's lanes
+//            hold the same ones.  The result leaves a lane with the scores of query row i for tokens 4g .. 4g+3.
+//   values   O^T = V^T P^T, dims x query rows, over 32 tokens: the weights of two blocks as they stand are operand B (tokens 4g .. 4g+3 of
+//            both), and the values' codes are stored so that a lane reads, as one vector, the same four tokens of dim / 16 elements.
+//   sums     of the weights, as they were rounded: an MFMA with ones.
+// Elements E2M1 become 16-bit ones, scaled, in v_cvt_scalef32_pk_*_fp4 (exact).  The softmax runs in one pass; its reference is raised, and
+// what has been summed scaled down, only when a score exceeds it by 2^kLag, so that most steps need nothing from another lane.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "st_launch.h"
+#include "st_lm_internal.h"
+#include "st_tiles.hpp"
+
+namespace st {
+
+typedef __attribute__((address_space(4))) const AttnDev ConstAttn;
+typedef __attribute__((address_space(4))) const AttnItem ConstAttnItem;
+typedef __attribute__((address_space(4))) const int32_t ConstInt;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));      // tensors ask no more of an address than their element's size
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+
+// A sequence's numbers, held to what the descriptor allows.
+struct Seq {
+  int first;      // row of its first new token
+  int n;          // new tokens, at most max_new
+  int length;     // tokens in the cache
+  int before;     // position of the first new token (negative: there are more new tokens than tokens)
+};
+__device__ __forceinline__ Seq sequence(ConstAttn& T, int seq) {
+  const int a = ((ConstInt*)T.first)[seq], b = ((ConstInt*)T.first)[seq + 1], len = ((ConstInt*)T.length)[seq];
+  const int64_t cap = (int64_t)T.table_pages << T.page_shift;
+  const int f0 = a < 0 ? 0 : a > T.max_tokens ? T.max_tokens : a, f1 = b < f0 ? f0 : b > T.max_tokens ? T.max_tokens : b;
+  const int length = len < 0 ? 0 : len > cap ? (int)cap : len;
+  const int all = f1 - f0, n = all < T.max_new ? all : T.max_new;
+  if (threadIdx.x == 0 && (f0 != a || f1 != b || length != len || n != all || all > length)) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_LENGTH);
+  return {f0, n, length, length - all};
+}
+// The page of token t (t >= 0, below the table's end), or -1.
+__device__ __forceinline__ int page_of(ConstAttn& T, int seq, int t) {
+  const int page = ((ConstInt*)T.table)[(int64_t)seq * T.table_pages + (t >> T.page_shift)];
+  return (uint32_t)page < (uint32_t)T.n_pages ? page : -1;
+}
+__device__ __forceinline__ const char* block_of(ConstAttn& T, int page, int head, int t, int block_bytes) {
+  const int in_page = t & ((1 << T.page_shift) - 1), blocks = 1 << (T.page_shift - 4);
+  return (const char*)T.pages + (int64_t)page * T.page_bytes + ((int64_t)head * blocks + (in_page >> 4)) * block_bytes;
+}
+
+// ---- elements and scales ----------------------------------------------------------------------------------------------
+template <int DT, int BYTE>
+__device__ __forceinline__ uint32_t widen(uint32_t codes, float scale) {      // byte BYTE's two elements, the lower one first
+  if constexpr (DT == ST_DT_BF16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, BYTE));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, BYTE));
+}
+// Scales above these count as these, so that no value is infinite (and weight 0 times it not a number).
+template <int DT> constexpr uint32_t kMostScale = DT == ST_DT_BF16 ? 252u : 140u;
+template <int DT>
+__device__ __forceinline__ float value_scale(uint32_t code) {
+  return __builtin_bit_cast(float, (code < kMostScale<DT> ? code : kMostScale<DT>) << 23);
+}
+template <int DT>
+__device__ __forceinline__ float key_scale(uint32_t code) {      // 255: not a number
+  const uint32_t held = code < kMostScale<DT> ? code : kMostScale<DT>;
+  return __builtin_bit_cast(float, code == 255u ? 0x7fc00000u : held << 23);
+}
+
+template <int DT>
+__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  if constexpr (DT == ST_DT_BF16) return pack16<DT>(a, b);
+  else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+}
+__device__ __forceinline__ float max_of_row(float v) {      // over the four lanes that hold a query row
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+
+// ---- one wavefront's rows over a stretch of tokens -----------------------------------------------------------------------
+template <int DT, int D, int R>
+struct Attend {
+  static constexpr int KW = D / 32;        // dwords of a key quarter; MFMAs per score block
+  static constexpr int VW = D / 32;        // dwords of four tokens' group of values
+  static constexpr int NE = D / 16;        // output blocks (elements of a group)
+  static constexpr int kBlock = attn_block_bytes(D);
+  // Weights are 2^(score - m) with m lagging behind the true maximum by at most kLag; in fp16 they are moved up to the end of the type's
+  // range, so that a weight has all its bits down to 2^-25 of the largest.
+  static constexpr float kLag = DT == ST_DT_BF16 ? 8.f : 5.f, kUp = DT == ST_DT_BF16 ? 0.f : 10.f;
+  static constexpr uint32_t kOnes = DT == ST_DT_BF16 ? 0x3f803f80u : 0x3c003c00u;
+  typedef Mma<DT, 16> Op;
+
+  u32x4 q[R][KW];
+  f32x4 acc[NE][R], sum[R];
+  float m[R];              // reference, less kUp; -inf: the row has seen no token yet
+  int lo[R], hi[R];        // tokens that the lane's rows see
+
+  struct Raw {
+    uint32_t k[2][KW], v[2][VW], ks[2], vs[2];
+    int bad;               // bit b: block b is on no page
+  };
+  struct Pages { int p[2]; };
+
+  __device__ __forceinline__ void clear() {
+    static_for<R>([&](auto J) {
+      constexpr int r = decltype(J)::value;
+      static_for<NE>([&](auto E) { acc[decltype(E)::value][r] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+      sum[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m[r] = -__builtin_inff();
+    });
+  }
+  // rows [row0, row0 + 16 R) of the sequence's new tokens x heads of a group: row = token * group + head
+  __device__ __forceinline__ void load_rows(ConstAttn& T, const Seq& S, int head, int row0, int lane) {
+    const int i = lane & 15, g = lane >> 4, rows = S.n * T.group;
+    static_for<R>([&](auto J) {
+      constexpr int r = decltype(J)::value;
+      const int row = row0 + r * 16 + i, j = row / T.group, h = row - j * T.group;
+      const bool real = row < rows;
+      const uint16_t* p = (const uint16_t*)T.q + (int64_t)(S.first + (real ? j : 0)) * T.ldq + (int64_t)(head * T.group + (real ? h : 0)) * D + g * (D / 4);
+      static_for<KW>([&](auto B) {
+        constexpr int b = decltype(B)::value;
+        q[r][b] = real ? *(const u32x4_any*)(p + 8 * b) : u32x4{0u, 0u, 0u, 0u};
+      });
+      const int pos = S.before + j;
+      hi[r] = !real ? -1 : T.causal ? pos : S.length - 1;
+      lo[r] = T.window ? pos - T.window + 1 : 0;
+    });
+  }
+  // the page of both blocks of step s; a block behind `last` takes the first one's
+  static __device__ __forceinline__ Pages look_up(ConstAttn& T, int seq, int s, int last) {
+    const int t = s * kAttnStep;
+    return {{page_of(T, seq, t), page_of(T, seq, t + 16 <= last ? t + 16 : t)}};
+  }
+  static __device__ __forceinline__ void fetch(ConstAttn& T, Raw& raw, int head, int s, int last, const Pages& pages, int lane) {
+    const int i = lane & 15, g = lane >> 4;
+    raw.bad = 0;
+    static_for<2>([&](auto B) {
+      constexpr int b = decltype(B)::value;
+      const int t = s * kAttnStep + (b && s * kAttnStep + 16 <= last ? 16 : 0), page = pages.p[b];
+      if (page < 0) raw.bad |= 1 << b;
+      const char* at = block_of(T, page < 0 ? 0 : page, head, t, kBlock);
+      const char *kp = at + (uint32_t)(i * (D / 2) + g * (D / 8)), *vp = at + (uint32_t)(8 * D + (i * 16 + 4 * g) * (D / 32));
+      if constexpr (D == 64) {
+        const u32x2 a = *(const u32x2*)kp, c = *(const u32x2*)vp;
+        raw.k[b][0] = a[0], raw.k[b][1] = a[1], raw.v[b][0] = c[0], raw.v[b][1] = c[1];
+      } else {
+        static_for<D / 128>([&](auto W) {
+          constexpr int w = decltype(W)::value;
+          const u32x4 a = *(const u32x4*)(kp + 16 * w), c = *(const u32x4*)(vp + 16 * w);
+          static_for<4>([&](auto X) { raw.k[b][4 * w + decltype(X)::value] = a[decltype(X)::value], raw.v[b][4 * w + decltype(X)::value] = c[decltype(X)::value]; });
+        });
+      }
+      const char* ks = at + (uint32_t)(16 * D + i * (D / 32) + (D == 64 ? g / 2 : D == 128 ? g : 2 * g));
+      if constexpr (D == 256) raw.ks[b] = *(const uint16_t*)ks;
+      else raw.ks[b] = *(const uint8_t*)ks;
+      raw.vs[b] = *(const uint32_t*)(at + (uint32_t)(16 * D + D / 2 + (D == 64 ? i / 8 : D == 128 ? i / 4 : i / 2) * 16 + 4 * g));
+    });
+  }
+
+  // Tokens [32 s, 32 s + 32).  MASK: some row does not see some of them.
+  template <bool MASK>
+  __device__ __forceinline__ void step(const Raw& raw, int s, int length, float scale, int lane) {
+    const int g = lane >> 4;
+    f32x4 score[2][R];
+    static_for<2>([&](auto B) {
+      constexpr int b = decltype(B)::value;
+      static_for<R>([&](auto J) { score[b][decltype(J)::value] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+      static_for<KW>([&](auto W) {
+        constexpr int w = decltype(W)::value;
+        const float sc = key_scale<DT>(D == 256 ? (w < KW / 2 ? raw.ks[b] & 255u : raw.ks[b] >> 8) : raw.ks[b]);
+        const uint32_t c = raw.k[b][w];
+        const u32x4 a = {widen<DT, 0>(c, sc), widen<DT, 1>(c, sc), widen<DT, 2>(c, sc), widen<DT, 3>(c, sc)};
+        static_for<R>([&](auto J) { score[b][decltype(J)::value] = Op::run(a, q[decltype(J)::value][w], score[b][decltype(J)::value]); });
+      });
+    });
+    float y[R][8];
+    bool above = false;
+    static_for<R>([&](auto J) {
+      constexpr int r = decltype(J)::value;
+      static_for<8>([&](auto X) {
+        constexpr int x = decltype(X)::value;
+        y[r][x] = __builtin_fmaf(score[x / 4][r][x % 4], scale, -m[r]);
+        if constexpr (MASK) {
+          const int t = s * kAttnStep + (x / 4) * 16 + 4 * g + x % 4;
+          const bool seen = (t <= hi[r]) & (t >= lo[r]) & !((raw.bad >> (x / 4)) & 1);
+          y[r][x] = seen ? y[r][x] : -__builtin_inff();
+        }
+      });
+      const float top = fmaxf(fmaxf(fmaxf(y[r][0], y[r][1]), fmaxf(y[r][2], y[r][3])), fmaxf(fmaxf(y[r][4], y[r][5]), fmaxf(y[r][6], y[r][7])));
+      above |= top > kLag + kUp;
+    });
+    if (__any(above)) {
+      static_for<R>([&](auto J) {
+        constexpr int r = decltype(J)::value;
+        float x8[8], top = -__builtin_inff();
+        static_for<8>([&](auto X) {
+          constexpr int x = decltype(X)::value;
+          x8[x] = score[x / 4][r][x % 4] * scale;
+          if constexpr (MASK) x8[x] = y[r][x] == -__builtin_inff() ? y[r][x] : x8[x];
+          top = fmaxf(top, x8[x]);
+        });
+        top = max_of_row(top) - kUp;
+        const float next = fmaxf(m[r], top), base = next == -__builtin_inff() ? 0.f : next;
+        const float down = __builtin_amdgcn_exp2f(m[r] - base);
+        m[r] = next;
+        static_for<8>([&](auto X) { y[r][decltype(X)::value] = x8[decltype(X)::value] - base; });
+        static_for<NE>([&](auto E) { acc[decltype(E)::value][r] *= down; });
+        sum[r] *= down;
+      });
+    }
+    u32x4 p[R];
+    static_for<R>([&](auto J) {
+      constexpr int r = decltype(J)::value;
+      static_for<4>([&](auto X) {
+        constexpr int x = decltype(X)::value;
+        p[r][x] = pack_pair<DT>(__builtin_amdgcn_exp2f(y[r][2 * x]), __builtin_amdgcn_exp2f(y[r][2 * x + 1]));
+      });
+      sum[r] = Op::run(u32x4{kOnes, kOnes, kOnes, kOnes}, p[r], sum[r]);
+    });
+    float vsc[8];
+    static_for<8>([&](auto X) {
+      constexpr int x = decltype(X)::value;
+      vsc[x] = value_scale<DT>((raw.vs[x / 4] >> (8 * (x % 4))) & 255u);
+      if constexpr (MASK) {                // what lies behind the sequence's end, or on no page, may be anything
+        const int t = s * kAttnStep + (x / 4) * 16 + 4 * g + x % 4;
+        vsc[x] = (t < length) & !((raw.bad >> (x / 4)) & 1) ? vsc[x] : 1.f;
+      }
+    });
+    // two elements of the group at a time: byte e2 of a token's part of the group
+    static_for<NE / 2>([&](auto E2) {
+      constexpr int e2 = decltype(E2)::value;
+      u32x4 a0, a1;
+      static_for<4>([&](auto X) {          // token pairs
+        constexpr int x = decltype(X)::value, b = x / 2, t0 = 2 * (x % 2);
+        constexpr int at0 = t0 * (D / 32) + e2, at1 = (t0 + 1) * (D / 32) + e2;
+        const uint32_t c0 = widen<DT, at0 % 4>(raw.v[b][at0 / 4], vsc[4 * b + t0]), c1 = widen<DT, at1 % 4>(raw.v[b][at1 / 4], vsc[4 * b + t0 + 1]);
+        a0[x] = __builtin_amdgcn_perm(c1, c0, 0x05040100u);
+        a1[x] = __builtin_amdgcn_perm(c1, c0, 0x07060302u);
+      });
+      static_for<R>([&](auto J) {
+        constexpr int r = decltype(J)::value;
+        acc[2 * e2][r] = Op::run(a0, p[r], acc[2 * e2][r]);
+        acc[2 * e2 + 1][r] = Op::run(a1, p[r], acc[2 * e2 + 1][r]);
+      });
+    });
+  }
+
+  // Steps begin, begin + STRIDE, ... before end; `last`: the last token that any row sees; tokens [all_lo, all_hi] are seen by all rows.
+  template <int STRIDE>
+  __device__ __forceinline__ void run(ConstAttn& T, int seq, int head, int length, int begin, int end, int last, int all_lo, int all_hi, int lane) {
+    if (begin >= end) return;
+    const float scale = T.scale;
+    const int final_step = end - 1;
+    auto held = [&](int s) { return s < final_step ? s : final_step; };      // what is fetched ahead stays inside
+    int bad = 0;
+    auto compute = [&](const Raw& raw, int s) {
+      bad |= raw.bad;
+      const int t = s * kAttnStep;
+      if (t >= all_lo && t + kAttnStep - 1 <= all_hi && raw.bad == 0) step<false>(raw, s, length, scale, lane);
+      else step<true>(raw, s, length, scale, lane);
+    };
+    Raw r0, r1;
+    fetch(T, r0, head, begin, last, look_up(T, seq, begin, last), lane);
+    Pages next = look_up(T, seq, held(begin + STRIDE), last);
+    for (int s = begin; s < end; s += 2 * STRIDE) {
+      fetch(T, r1, head, held(s + STRIDE), last, next, lane);
+      next = look_up(T, seq, held(s + 2 * STRIDE), last);
+      compute(r0, s);
+      if (s + STRIDE >= end) break;
+      fetch(T, r0, head, held(s + 2 * STRIDE), last, next, lane);
+      next = look_up(T, seq, held(s + 3 * STRIDE), last);
+      compute(r1, s + STRIDE);
+    }
+    if (bad && lane == 0) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_PAGE);
+  }
+};
+
+// The tokens that rows [row0, row1) of a sequence see: any of them, and all of them.
+struct Seen { int lo, hi, all_lo, all_hi; };
+__device__ __forceinline__ Seen seen_by(ConstAttn& T, const Seq& S, int row0, int row1) {
+  const int p0 = S.before + row0 / T.group, p1 = S.before + (row1 - 1) / T.group;
+  Seen s;
+  s.hi = T.causal ? p1 : S.length - 1;
+  s.all_hi = T.causal ? p0 : S.length - 1;
+  s.lo = T.window && p0 - T.window + 1 > 0 ? p0 - T.window + 1 : 0;
+  s.all_lo = T.window && p1 - T.window + 1 > 0 ? p1 - T.window + 1 : 0;
+  if (T.n_pages == 0) s.hi = -1;
+  return s;
+}
+
+template <int DT, int W>
+__device__ __forceinline__ void store_out(ConstAttn& T, const Seq& S, int head, int row, int dim, int D, const float* v) {
+  const int j = row / T.group, h = row - j * T.group;
+  uint16_t* p = (uint16_t*)T.out + (int64_t)(S.first + j) * T.ldo + (int64_t)(head * T.group + h) * D + dim;
+  if constexpr (W == 8) *(u32x4_any*)p = u32x4{pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3]), pack_pair<DT>(v[4], v[5]), pack_pair<DT>(v[6], v[7])};
+  else *(u32x2_any*)p = u32x2{pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3])};
+}
+
+// ---- each wavefront its own rows ----------------------------------------------------------------------------------------
+template <int DT, int D, int R>
+__global__ __launch_bounds__(kAttnRowWaves * 64) void st_attn_rows_kernel(const AttnDev* table, const AttnItem* items) {
+  const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
+  ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
+  const int seq = (int)ci.seq, head = (int)ci.head;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const Seq S = sequence(T, seq);
+  const int rows = S.n * T.group, row0 = ((int)ci.part * kAttnRowWaves + wave) * 16 * R;
+  if (row0 >= rows) return;
+  const int row1 = row0 + 16 * R < rows ? row0 + 16 * R : rows;
+  const Seen see = seen_by(T, S, row0, row1);
+  Attend<DT, D, R> a;
+  a.clear();
+  a.load_rows(T, S, head, row0, lane);
+  if (see.hi >= see.lo) a.template run<1>(T, seq, head, S.length, see.lo / kAttnStep, see.hi / kAttnStep + 1, see.hi, see.all_lo, see.all_hi, lane);
+  const int i = lane & 15, g = lane >> 4;
+  static_for<R>([&](auto J) {
+    constexpr int r = decltype(J)::value;
+    const int row = row0 + r * 16 + i;
+    const float total = a.sum[r][0], inv = total == 0.f ? 0.f : 1.f / total;
+    if (row < rows) {
+      static_for<4>([&](auto X) {
+        constexpr int x = decltype(X)::value;
+        float v[D / 16];
+        static_for<D / 16>([&](auto E) { v[decltype(E)::value] = a.acc[decltype(E)::value][r][x] * inv; });
+        const int dim = (4 * g + x) * (D / 16);
+        if constexpr (D == 64) store_out<DT, 4>(T, S, head, row, dim, D, v);
+        else static_for<D / 128>([&](auto C) { store_out<DT, 8>(T, S, head, row, dim + 8 * decltype(C)::value, D, v + 8 * decltype(C)::value); });
+      });
+    }
+  });
+}
+
+// ---- a workgroup's wavefronts take turns over a stretch of tokens -------------------------------------------------------
+// The wavefronts' results meet in LDS; where a sequence has several stretches their results meet in memory, and the last workgroup to
+// arrive joins them in order.
+template <int DT, int D, int R>
+__global__ __launch_bounds__(kAttnTokenWaves * 64) void st_attn_tokens_kernel(const AttnDev* table, const AttnItem* items) {
+  constexpr int W = kAttnTokenWaves, THREADS = W * 64, ROWS = 16 * R;
+  constexpr int DP = D < 128 ? D : 128, PASS = D / DP, EP = DP / 16, kPitch = DP + 4;       // dims per pass
+  __shared__ __align__(16) float part[W][16][kPitch];
+  __shared__ float wave_m[W][ROWS], wave_l[W][ROWS], weight[kAttnMaxSplit][ROWS], inverse[ROWS];
+  __shared__ uint32_t flag;
+  const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
+  ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
+  const int seq = (int)ci.seq, head = (int)ci.head, row_tile = (int)ci.part / T.split, stretch = (int)ci.part - row_tile * T.split;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+  const Seq S = sequence(T, seq);
+  const int rows = S.n * T.group, row0 = row_tile * ROWS;
+  if (row0 >= rows) return;
+  const int row1 = row0 + ROWS < rows ? row0 + ROWS : rows;
+  const Seen see = seen_by(T, S, row0, row1);
+  const int s_lo = see.lo / kAttnStep, steps = see.hi >= see.lo ? see.hi / kAttnStep + 1 - s_lo : 0;
+  const int active = steps > T.chunk ? (steps + T.chunk - 1) / T.chunk : 1;      // stretches that there are
+  if (stretch >= active) return;
+  const int begin = s_lo + stretch * T.chunk, end = stretch + 1 < active ? begin + T.chunk : s_lo + steps;
+
+  Attend<DT, D, R> a;
+  a.clear();
+  a.load_rows(T, S, head, row0, lane);
+  a.template run<W>(T, seq, head, S.length, begin + wave, end, see.hi, see.all_lo, see.all_hi, lane);
+
+  // all wavefronts' sums to one reference
+  static_for<R>([&](auto J) {
+    constexpr int r = decltype(J)::value;
+    if (g == 0) wave_m[wave][r * 16 + i] = a.m[r];
+  });
+  __syncthreads();
+  float ref[R];
+  static_for<R>([&](auto J) {
+    constexpr int r = decltype(J)::value;
+    float top = -__builtin_inff();
+    for (int w = 0; w < W; ++w) top = fmaxf(top, wave_m[w][r * 16 + i]);
+    ref[r] = top;
+    const float down = a.m[r] == -__builtin_inff() && a.sum[r][0] == 0.f ? 0.f : __builtin_amdgcn_exp2f(a.m[r] - top);
+    static_for<D / 16>([&](auto E) { a.acc[decltype(E)::value][r] *= down; });
+    if (g == 0) wave_l[wave][r * 16 + i] = a.sum[r][0] * down;
+  });
+  __syncthreads();
+  if (tid < ROWS) {
+    float total = 0.f;
+    for (int w = 0; w < W; ++w) total += wave_l[w][tid];
+    wave_l[0][tid] = total;
+    inverse[tid] = total == 0.f ? 0.f : 1.f / total;
+  }
+  const int64_t tile = ((int64_t)seq * T.kv_heads + head) * T.row_tiles + row_tile;
+  const int64_t slots = (int64_t)T.n_seqs * T.kv_heads * T.row_tiles * T.split;
+  float* parts = T.ws + tile * T.split * (ROWS * D);
+  float* stats = T.ws + slots * (ROWS * D) + tile * T.split * (2 * ROWS);
+  __syncthreads();
+  static_for<R * PASS>([&](auto RP) {
+    constexpr int r = decltype(RP)::value / PASS, pass = decltype(RP)::value % PASS;
+    static_for<4>([&](auto X) {
+      constexpr int x = decltype(X)::value;
+      static_for<EP / 4>([&](auto C) {
+        constexpr int c = decltype(C)::value, e = pass * EP + 4 * c;
+        *(f32x4*)&part[wave][i][(4 * g + x) * EP + 4 * c] = f32x4{a.acc[e][r][x], a.acc[e + 1][r][x], a.acc[e + 2][r][x], a.acc[e + 3][r][x]};
+      });
+    });
+    __syncthreads();
+    for (int at = tid; at < 16 * DP / 4; at += THREADS) {
+      const int row16 = at / (DP / 4), c = at % (DP / 4) * 4, row = r * 16 + row16;
+      f32x4 v = *(const f32x4*)&part[0][row16][c];
+#pragma unroll
+      for (int w = 1; w < W; ++w) v += *(const f32x4*)&part[w][row16][c];
+      const int dim = c / EP * (D / 16) + pass * EP + c % EP;
+      if (row0 + row < row1) {
+        if (active == 1) {
+          const float f = inverse[row];
+          const float o[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
+          store_out<DT, 4>(T, S, head, row0 + row, dim, D, o);
+        } else {
+          const __amdgpu_buffer_rsrc_t rs = make_rsrc(parts + (int64_t)stretch * (ROWS * D), ROWS * D * 4);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, (row * D + dim) * 4, 0, kAuxDeviceCoherent);
+        }
+      }
+    }
+    __syncthreads();
+  });
+  if (active == 1) return;
+  const __amdgpu_buffer_rsrc_t rstat = make_rsrc(stats, (uint32_t)T.split * 2 * ROWS * 4);
+  if (wave == 0) {
+    static_for<R>([&](auto J) {
+      constexpr int r = decltype(J)::value;
+      if (g == 0) {
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, ref[r]), rstat, (stretch * 2 * ROWS + r * 16 + i) * 4, 0, kAuxDeviceCoherent);
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, wave_l[0][r * 16 + i]), rstat, (stretch * 2 * ROWS + ROWS + r * 16 + i) * 4, 0, kAuxDeviceCoherent);
+      }
+    });
+  }
+  __builtin_amdgcn_s_waitcnt(0);      // this thread's stores have been written through
+  __syncthreads();
+  if (tid == 0) {
+    const uint32_t old = __hip_atomic_fetch_add(&T.counters[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const uint32_t is_last = old == (uint32_t)(active - 1);
+    if (is_last) __hip_atomic_store(&T.counters[tile], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    flag = is_last;
+  }
+  __syncthreads();
+  if (flag == 0u) return;
+  if (tid < ROWS) {
+    float top = -__builtin_inff(), total = 0.f;
+    for (int s = 0; s < active; ++s) {
+      const float ms = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rstat, (s * 2 * ROWS + tid) * 4, 0, kAuxDeviceCoherent));
+      weight[s][tid] = ms;
+      top = fmaxf(top, ms);
+    }
+    for (int s = 0; s < active; ++s) {
+      const float l = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rstat, (s * 2 * ROWS + ROWS + tid) * 4, 0, kAuxDeviceCoherent));
+      const float w = weight[s][tid] == -__builtin_inff() && l == 0.f ? 0.f : __builtin_amdgcn_exp2f(weight[s][tid] - top);
+      weight[s][tid] = w;
+      total += w * l;
+    }
+    inverse[tid] = total == 0.f ? 0.f : 1.f / total;
+  }
+  __syncthreads();
+  const __amdgpu_buffer_rsrc_t rp = make_rsrc(parts, (uint32_t)T.split * ROWS * D * 4);
+  for (int at = tid; at < (row1 - row0) * (D / 4); at += THREADS) {
+    const int row = at / (D / 4), dim = at % (D / 4) * 4;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < active; s0 += 8) {
+      f32x4 one[8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        one[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rp, (int)(s0 + s < active ? (uint32_t)(((s0 + s) * ROWS + row) * D + dim) * 4u : kInvalidOffset), 0, kAuxDeviceCoherent));
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        if (s0 + s < active) v += one[s] * weight[s0 + s][row];
+    }
+    const float f = inverse[row];
+    const float o[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
+    store_out<DT, 4>(T, S, head, row0 + row, dim, D, o);
+  }
+}
+
+// ---- into the cache and out of it ---------------------------------------------------------------------------------------
+// dim / 8 lanes to a token's head: each has eight elements of the key and of the value.  With many new tokens 16 of them, of one head,
+// lie side by side, as they do in a block.
+template <int DT>
+__device__ __forceinline__ void encode8(const u32x4 in, int lane, uint32_t& codes, uint32_t& scale, bool& finite) {
+  float v[8], most = 0.f;
+  finite = true;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    v[e] = unpack16<DT>(in[e / 2], e & 1);
+    finite &= __builtin_fabsf(v[e]) < __builtin_inff();
+    most = fmaxf(most, __builtin_fabsf(v[e]));
+  }
+  most = fmaxf(most, __shfl_xor(most, 1));      // four lanes to a group of 32
+  most = fmaxf(most, __shfl_xor(most, 2));
+  const uint32_t bits = __builtin_bit_cast(uint32_t, most);
+  int e = (int)(bits >> 23) - 2 + ((bits & 0x7fffffu) > 0x400000u ? 1 : 0);
+  e = e < 1 ? 1 : e > 252 ? 252 : e;
+  scale = (uint32_t)e;
+  const float f = __builtin_bit_cast(float, scale << 23);
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], f, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], f, 3);
+  codes = c;
+}
+
+template <int DT, int D, bool READ>
+__global__ __launch_bounds__(256) void st_attn_move_kernel(const AttnDev* table, const AttnItem* items) {
+  constexpr int LPT = D / 8, kBlock = attn_block_bytes(D);
+  const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
+  ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
+  const int seq = (int)ci.seq, lane = (int)threadIdx.x & 63, c = (int)threadIdx.x % LPT;
+  const Seq S = sequence(T, seq);
+  const int th = (int)ci.part * attn_move_count(D) + (int)threadIdx.x / LPT;
+  int j, head;
+  if (T.max_new >= 16) {
+    const int group = th / 16;
+    head = group % T.kv_heads;
+    j = group / T.kv_heads * 16 + th % 16;
+  } else {
+    j = th / T.kv_heads;
+    head = th - j * T.kv_heads;
+  }
+  const bool real = j < S.n;
+  const int pos = S.before + j;
+  int page = -1;
+  if (real && pos >= 0) {
+    const int p = T.table[(int64_t)seq * T.table_pages + (pos >> T.page_shift)];
+    if ((uint32_t)p < (uint32_t)T.n_pages) page = p;
+    else if (c == 0) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_PAGE);
+  }
+  const int t = pos & 15;
+  char* at = const_cast<char*>(block_of(T, page < 0 ? 0 : page, head, pos, kBlock));
+  char *kp = at + t * (D / 2) + c * 4, *ks = at + 16 * D + t * (D / 32) + c / 4, *vs = at + 16 * D + D / 2 + (c / 4) * 16 + t;
+  char* vp = at + 8 * D + (D == 64 ? (2 * c * 16 + t) * 2 : D == 128 ? (c * 16 + t) * 4 : (c / 2 * 16 + t) * 8 + c % 2 * 4);
+  const int64_t row = S.first + (real ? j : 0);
+  if constexpr (!READ) {
+    u32x4 k = {0u, 0u, 0u, 0u}, v = k;
+    if (page >= 0) {
+      k = *(const u32x4_any*)((const uint16_t*)T.k + row * T.ldk + head * D + c * 8);
+      v = *(const u32x4_any*)((const uint16_t*)T.v + row * T.ldv + head * D + c * 8);
+    }
+    uint32_t kc, kscale, vc, vscale;
+    bool kfin, vfin;
+    encode8<DT>(k, lane, kc, kscale, kfin);
+    encode8<DT>(v, lane, vc, vscale, vfin);
+    const uint64_t odd = __ballot(!(kfin && vfin)) >> (lane & ~(LPT - 1));
+    if ((odd & (((uint64_t)1 << LPT) - 1)) != 0) kc = vc = 0u, kscale = 255u, vscale = 1u;
+    if (page < 0) return;
+    *(uint32_t*)kp = kc;
+    if constexpr (D == 64) {
+      *(uint16_t*)vp = (uint16_t)vc;
+      *(uint16_t*)(vp + 32) = (uint16_t)(vc >> 16);
+    } else {
+      *(uint32_t*)vp = vc;
+    }
+    if (c % 4 == 0) {
+      *ks = (char)kscale;
+      *vs = (char)vscale;
+    }
+  } else {
+    if (!real) return;
+    u32x4 k = {0u, 0u, 0u, 0u}, v = k;
+    if (page >= 0) {
+      const uint32_t kc = *(const uint32_t*)kp;
+      uint32_t vc;
+      if constexpr (D == 64) vc = *(const uint16_t*)vp | (uint32_t)*(const uint16_t*)(vp + 32) << 16;
+      else vc = *(const uint32_t*)vp;
+      const float kf = key_scale<DT>(*(const uint8_t*)ks), vf = value_scale<DT>(*(const uint8_t*)vs);
+      k = u32x4{widen<DT, 0>(kc, kf), widen<DT, 1>(kc, kf), widen<DT, 2>(kc, kf), widen<DT, 3>(kc, kf)};
+      v = u32x4{widen<DT, 0>(vc, vf), widen<DT, 1>(vc, vf), widen<DT, 2>(vc, vf), widen<DT, 3>(vc, vf)};
+    }
+    *(u32x4_any*)((uint16_t*)T.k_out + row * T.ldk + head * D + c * 8) = k;
+    *(u32x4_any*)((uint16_t*)T.v_out + row * T.ldv + head * D + c * 8) = v;
+  }
+}
+
+// ---- launches -------------------------------------------------------------------------------------------------------------
+template <int DT, int D>
+static hipError_t launch_kind(int kind, unsigned blocks, void* stream, const AttnDev* table, const AttnItem* items) {
+  switch (kind) {
+    case 0: return launch(st_attn_tokens_kernel<DT, D, 1>, blocks, kAttnTokenWaves * 64, stream, table, items);
+    case 1: return launch(st_attn_tokens_kernel<DT, D, 2>, blocks, kAttnTokenWaves * 64, stream, table, items);
+    case 2: return launch(st_attn_rows_kernel<DT, D, 2>, blocks, kAttnRowWaves * 64, stream, table, items);
+    case 3:
+      if constexpr (D <= 128) return launch(st_attn_rows_kernel<DT, D, 4>, blocks, kAttnRowWaves * 64, stream, table, items);
+  }
+  return hipErrorInvalidValue;
+}
+template <int DT>
+static hipError_t launch_dim(int dim, int kind, unsigned blocks, void* stream, const AttnDev* table, const AttnItem* items) {
+  return dim == 64 ? launch_kind<DT, 64>(kind, blocks, stream, table, items) : dim == 128 ? launch_kind<DT, 128>(kind, blocks, stream, table, items)
+                                                                                          : launch_kind<DT, 256>(kind, blocks, stream, table, items);
+}
+int launch_attn(int dtype, int dim, int kind, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream) {
+  if (n_items <= 0) return 0;
+  return (int)(dtype == ST_DT_BF16 ? launch_dim<ST_DT_BF16>(dim, kind, (unsigned)n_items, stream, table_dev, items_dev)
+                                   : launch_dim<ST_DT_F16>(dim, kind, (unsigned)n_items, stream, table_dev, items_dev));
+}
+
+template <int DT, bool READ>
+static hipError_t launch_move(int dim, unsigned blocks, void* stream, const AttnDev* table, const AttnItem* items) {
+  auto kernel = dim == 64 ? st_attn_move_kernel<DT, 64, READ> : dim == 128 ? st_attn_move_kernel<DT, 128, READ> : st_attn_move_kernel<DT, 256, READ>;
+  return launch(kernel, blocks, 256, stream, table, items);
+}
+int launch_attn_move(bool read, int dtype, int dim, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream) {
+  if (n_items <= 0) return 0;
+  const auto run = dtype == ST_DT_BF16 ? (read ? launch_move<ST_DT_BF16, true> : launch_move<ST_DT_BF16, false>)
+                                       : (read ? launch_move<ST_DT_F16, true> : launch_move<ST_DT_F16, false>);
+  return (int)run(dim, (unsigned)n_items, stream, table_dev, items_dev);
+}
+
+}  // namespace st

@@ -1,6 +1,7 @@
 // What the host sources of the operators of language models share.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <stdint.h>
 
 namespace st {
 
@@ -22,5 +23,20 @@ struct OnDevice {
   OnDevice(const OnDevice&) = delete;
   OnDevice& operator=(const OnDevice&) = delete;
 };
+
+// What a matrix of rows spans; whether two of them share a byte.
+struct Span {
+  uintptr_t at;
+  int64_t rows, row_bytes, turn;     // turn: bytes from a row to the next
+  uintptr_t end() const { return at + (uintptr_t)((rows - 1) * turn + row_bytes); }
+};
+inline bool overlap(const Span& a, const Span& b) {
+  if (a.rows <= 0 || b.rows <= 0 || a.at >= b.end() || b.at >= a.end()) return false;
+  if (a.turn == b.turn) {             // columns of one matrix that lie beside each other
+    const int64_t off = (((int64_t)b.at - (int64_t)a.at) % a.turn + a.turn) % a.turn;      // where b's rows start in a's
+    if (off >= a.row_bytes && off + b.row_bytes <= a.turn) return false;
+  }
+  return true;
+}
 
 }  // namespace st

@@ -51,4 +51,52 @@ struct MatmulItem { uint32_t tenant, tile_m, tile_n, slice; };
 
 int launch_matmul(int dtype, int shape, const MatmulDev* table_dev, const MatmulItem* items_dev, int64_t n_items, void* stream);
 
+// ---- attention over a paged cache in 4 bits ---------------------------------------------------------------------------
+// How an st_attn_run divides the work (see st_attn.hip).  kByTokens: a workgroup's wavefronts take the tokens of a stretch in turn, all
+// for the same rows, of which there are 16 R; kByRows: each wavefront takes 16 R rows of its own and all the tokens they see.
+constexpr int kAttnBlock = 16;           // tokens per cache block
+constexpr int kAttnStep = 32;            // tokens per step of a wavefront
+constexpr int kAttnTokenWaves = 8, kAttnRowWaves = 4;
+constexpr int kAttnMaxSplit = 64;
+struct AttnKind { bool by_rows; int R; };
+constexpr AttnKind kAttnKinds[] = {{false, 1}, {false, 2}, {true, 2}, {true, 4}};
+constexpr int kNumAttnKinds = (int)(sizeof(kAttnKinds) / sizeof(kAttnKinds[0]));
+
+// Bytes of a block of 16 tokens of one head, and where its parts begin.
+constexpr int attn_block_bytes(int dim) { return kAttnBlock * (dim + dim / 16); }
+
+struct AttnDev {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  void* k_out;
+  void* v_out;
+  void* pages;
+  const int32_t* table;
+  const int32_t* first;
+  const int32_t* length;
+  float* ws;             // partial results: [tile][split][rows][dim], then their maxima and sums, [tile][split][2][rows]
+  uint32_t* counters;    // one arrival counter per tile, zero between runs
+  uint32_t* status;      // ST_ATTN_BAD_* that runs have met
+  int64_t ldq, ldk, ldv, ldo;
+  int64_t page_bytes;
+  int32_t heads, kv_heads, group, n_seqs;
+  int32_t max_tokens, max_new, n_pages, page_shift;
+  int32_t table_pages, window, causal;
+  float scale;           // times log2(e)
+  int32_t row_tiles;     // per sequence and key head
+  int32_t split, chunk;  // at most `split` stretches of `chunk` steps
+  int32_t pad;
+};
+static_assert(sizeof(AttnDev) == 208, "a multiple of 16 bytes for launch_poke");
+
+struct AttnItem { uint32_t tenant, seq, head, part; };   // part: row tile * split + stretch, or the stretch of new tokens
+
+int launch_attn(int dtype, int dim, int kind, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream);
+// new tokens into the cache, or (read) out of it; part: the stretch of attn_move_count() of a sequence's new tokens x key heads
+int launch_attn_move(bool read, int dtype, int dim, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream);
+// token-heads that a workgroup of these moves
+constexpr int attn_move_count(int dim) { return 256 / (dim / 8); }
+
 }  // namespace st

@@ -34,21 +34,6 @@ constexpr uint32_t kResiduals = ST_EPI_RESIDUAL | ST_EPI_RESIDUAL_LAST;
 
 int64_t row_of(int64_t ld, int64_t dense) { return ld ? ld : dense; }
 
-// What a matrix of rows spans; whether two of them share a byte.
-struct Span {
-  uintptr_t at;
-  int64_t rows, row_bytes, turn;     // turn: bytes from a row to the next
-  uintptr_t end() const { return at + (uintptr_t)((rows - 1) * turn + row_bytes); }
-};
-bool overlap(const Span& a, const Span& b) {
-  if (a.rows <= 0 || b.rows <= 0 || a.at >= b.end() || b.at >= a.end()) return false;
-  if (a.turn == b.turn) {             // columns of one matrix that lie beside each other
-    const int64_t off = (((int64_t)b.at - (int64_t)a.at) % a.turn + a.turn) % a.turn;      // where b's rows start in a's
-    if (off >= a.row_bytes && off + b.row_bytes <= a.turn) return false;
-  }
-  return true;
-}
-
 st_status validate_sizes(const st_matmul_desc& d, int t) {
   if (d.M < 0 || d.N <= 0 || d.K <= 0) return fail(ST_ERR_INVALID_ARG, "tenant %d: N and K must be positive and M not negative", t);
   if (d.in_dtype != ST_DT_F32 && d.in_dtype != ST_DT_BF16 && d.in_dtype != ST_DT_F16)

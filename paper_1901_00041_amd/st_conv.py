@@ -29,7 +29,9 @@ EXPORTS = ["st_conv_plan", "st_conv_run", "st_conv_run_noalloc", "st_conv_noallo
            "st_launch_empty", "st_launch_copy", "st_status_string", "st_last_error_message",
            # include/st_lm.h (bound in st_lm.py)
            "st_matmul_plan", "st_matmul_run", "st_matmul_rebind_all", "st_matmul_get_info", "st_matmul_get_tenant_info", "st_matmul_destroy",
-           "st_matmul_tile_shape", "st_matmul_tile_count"]
+           "st_matmul_tile_shape", "st_matmul_tile_count",
+           "st_attn_page_bytes", "st_attn_plan", "st_attn_append", "st_attn_read", "st_attn_run", "st_attn_rebind_all", "st_attn_status",
+           "st_attn_get_info", "st_attn_destroy"]
 
 
 class st_conv_desc(ctypes.Structure):

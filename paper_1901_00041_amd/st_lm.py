@@ -9,6 +9,8 @@ from . import st_conv as sc
 from .st_conv import DTYPE_CODE, ST_EPI_RELU, ST_EPI_RESIDUAL, StError, _check, _ptr, _stream, plan_opts, st_plan_opts  # noqa: F401
 
 ST_EPI_BIAS, ST_EPI_GELU, ST_EPI_GELU_TANH, ST_EPI_SILU, ST_EPI_RESIDUAL_LAST = 4, 8, 16, 32, 64
+ST_ATTN_CAUSAL = 1
+ST_ATTN_BAD_PAGE, ST_ATTN_BAD_LENGTH = 1, 2
 
 
 class st_matmul_desc(ctypes.Structure):
@@ -25,6 +27,18 @@ class st_matmul_tenant_info(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("tile_cfg", "MT", "NT", "tiles_m", "tiles_n", "split_k")] + [("item_count", ctypes.c_int64)]
 
 
+class st_attn_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("heads", "kv_heads", "head_dim", "dtype", "n_seqs", "max_tokens", "max_new", "n_pages", "page_tokens",
+                                              "table_pages", "window")] + \
+               [("flags", ctypes.c_uint32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("ldq", "ldk", "ldv", "ldo")] + \
+               [(n, ctypes.c_void_p) for n in ("q", "k", "v", "out", "k_out", "v_out", "pages", "table", "first", "length")]
+
+
+class st_attn_info(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_tenants", "host_only", "launches", "reserved")] + [(n, ctypes.c_int64) for n in ("n_items", "workspace_bytes")]
+
+
 _bound = False
 
 
@@ -33,13 +47,17 @@ def lib() -> ctypes.CDLL:
     global _bound
     L = sc.lib()
     if not _bound:
-        vp, i32, P = ctypes.c_void_p, ctypes.c_int32, ctypes.POINTER
+        vp, i32, i64, P = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.POINTER
         for name, args in (("st_matmul_plan", [P(st_matmul_desc), i32, P(st_plan_opts), P(vp)]), ("st_matmul_run", [vp, vp]),
                            ("st_matmul_rebind_all", [vp, P(st_matmul_desc), i32, vp]), ("st_matmul_get_info", [vp, P(st_matmul_plan_info)]),
                            ("st_matmul_get_tenant_info", [vp, i32, P(st_matmul_tenant_info)]), ("st_matmul_tile_shape", [i32, P(i32), P(i32)]),
-                           ("st_matmul_tile_count", [])):
+                           ("st_matmul_tile_count", []),
+                           ("st_attn_plan", [P(st_attn_desc), i32, P(st_plan_opts), P(vp)]), ("st_attn_append", [vp, vp]), ("st_attn_read", [vp, vp]),
+                           ("st_attn_run", [vp, vp]), ("st_attn_rebind_all", [vp, P(st_attn_desc), i32, vp]), ("st_attn_status", [vp, P(i32)]),
+                           ("st_attn_get_info", [vp, P(st_attn_info)])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, i32
-        for name in ("st_matmul_destroy",):
+        L.st_attn_page_bytes.argtypes, L.st_attn_page_bytes.restype = [P(st_attn_desc)], i64
+        for name in ("st_matmul_destroy", "st_attn_destroy"):
             getattr(L, name).argtypes, getattr(L, name).restype = [vp], None
         _bound = True
     return L
@@ -66,6 +84,10 @@ class _Owned:
 
 class MatmulPlan(_Owned):
     _destroy = "st_matmul_destroy"
+
+
+class AttnPlan(_Owned):
+    _destroy = "st_attn_destroy"
 
 
 def _run(name: str, plan: _Owned, stream) -> None:
@@ -131,3 +153,60 @@ def st_matmul_tile_shape(index: int):
 
 def st_matmul_tile_count() -> int:
     return lib().st_matmul_tile_count()
+
+
+# ---- attention over a paged cache in 4 bits -----------------------------------------------------------------------
+def make_attn_desc(heads, kv_heads, head_dim, dtype, n_seqs, max_tokens, max_new, n_pages, page_tokens, table_pages, pages=None, table=None, first=None,
+                   length=None, q=None, k=None, v=None, out=None, k_out=None, v_out=None, scale=1.0, window=0, flags=0, ldq=0, ldk=0, ldv=0,
+                   ldo=0) -> st_attn_desc:
+    d = st_attn_desc()
+    d.heads, d.kv_heads, d.head_dim, d.dtype = heads, kv_heads, head_dim, DTYPE_CODE.get(dtype, dtype)
+    d.n_seqs, d.max_tokens, d.max_new = n_seqs, max_tokens, max_new
+    d.n_pages, d.page_tokens, d.table_pages = n_pages, page_tokens, table_pages
+    d.window, d.flags, d.scale, d.reserved = window, flags, scale, 0
+    d.ldq, d.ldk, d.ldv, d.ldo = ldq, ldk, ldv, ldo
+    d.q, d.k, d.v, d.out, d.k_out, d.v_out = (_ptr(t) for t in (q, k, v, out, k_out, v_out))
+    d.pages, d.table, d.first, d.length = (_ptr(t) for t in (pages, table, first, length))
+    return d
+
+
+def st_attn_page_bytes(desc: st_attn_desc) -> int:
+    return int(lib().st_attn_page_bytes(ctypes.byref(desc)))
+
+
+def st_attn_plan(descs: Sequence[st_attn_desc], opts: Optional[st_plan_opts] = None, keep=None) -> AttnPlan:
+    arr, n = _array(st_attn_desc, descs)
+    out = ctypes.c_void_p()
+    _check(lib().st_attn_plan(arr, n, ctypes.byref(opts) if opts is not None else None, ctypes.byref(out)), "st_attn_plan")
+    return AttnPlan(out.value, keep)
+
+
+def st_attn_append(plan: AttnPlan, stream=None) -> None:
+    _run("st_attn_append", plan, stream)
+
+
+def st_attn_read(plan: AttnPlan, stream=None) -> None:
+    _run("st_attn_read", plan, stream)
+
+
+def st_attn_run(plan: AttnPlan, stream=None) -> None:
+    _run("st_attn_run", plan, stream)
+
+
+def st_attn_rebind_all(plan: AttnPlan, descs: Sequence[st_attn_desc], stream=None, keep=None) -> None:
+    arr, n = _array(st_attn_desc, descs)
+    _check(lib().st_attn_rebind_all(plan.handle, arr, n, _stream(stream)), "st_attn_rebind_all")
+    if keep is not None:
+        plan._keep = (plan._keep, keep)
+
+
+def st_attn_status(plan: AttnPlan) -> int:
+    out = ctypes.c_int32()
+    _check(lib().st_attn_status(plan.handle, ctypes.byref(out)), "st_attn_status")
+    return out.value
+
+
+def st_attn_get_info(plan: AttnPlan) -> st_attn_info:
+    out = st_attn_info()
+    _check(lib().st_attn_get_info(plan.handle, ctypes.byref(out)), "st_attn_get_info")
+    return out
