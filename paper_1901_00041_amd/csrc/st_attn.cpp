@@ -96,9 +96,7 @@ int most_steps(const st_attn_desc& d) {      // that a row tile of single tokens
 // Few rows: the tokens are divided among wavefronts and workgroups; else the rows are.
 int kind_of(const st_attn_desc& d) {
   const int rows = most_rows(d);
-  if (rows <= 16) return 0;
-  if (rows <= 32) return 1;
-  return d.head_dim <= 128 ? 3 : 2;
+  return rows <= 16 ? kAttnTokens1 : rows <= 32 ? kAttnTokens2 : kAttnRows;
 }
 
 st_status upload(st_attn* p) {
@@ -108,10 +106,10 @@ st_status upload(st_attn* p) {
   size_t all_tiles = 0, all_floats = 0;
   for (size_t t = 0; t < n; ++t) {
     const AttnDev& T = p->tenants[t];
-    const AttnKind& K = kAttnKinds[kind_of(p->descs[t])];
-    if (K.by_rows || T.split <= 1) continue;
+    const int kind = kind_of(p->descs[t]);
+    if (kind == kAttnRows || T.split <= 1) continue;
     tiles[t] = (size_t)T.n_seqs * T.kv_heads * T.row_tiles;
-    floats[t] = tiles[t] * T.split * (size_t)(16 * K.R) * (size_t)(p->descs[t].head_dim + 2);
+    floats[t] = tiles[t] * T.split * (size_t)(16 * attn_blocks(kind, p->descs[t].head_dim)) * (size_t)(p->descs[t].head_dim + 2);
     all_tiles += tiles[t];
     all_floats += floats[t];
   }
@@ -148,7 +146,7 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
   double tiles = 0;      // of tenants whose tokens are divided, all together
   for (int t = 0; t < n; ++t) {
     const st_attn_desc& d = descs[t];
-    const AttnKind& K = kAttnKinds[kind_of(d)];
+    const int kind = kind_of(d);
     AttnDev& T = p->tenants[t];
     set_pointers(T, d);
     T.heads = d.heads; T.kv_heads = d.kv_heads; T.group = d.heads / d.kv_heads;
@@ -158,18 +156,21 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
     T.page_shift = __builtin_ctz((unsigned)d.page_tokens);
     T.page_bytes = page_bytes(d);
     T.table_pages = d.table_pages; T.window = d.window; T.causal = (d.flags & ST_ATTN_CAUSAL) != 0;
-    T.scale = d.scale * 1.44269504088896340736f;
-    T.row_tiles = cdiv(most_rows(d), (K.by_rows ? kAttnRowWaves : 1) * 16 * K.R);
+    // hidden tokens get the score -inf, which has to stay that under the scale: a negative one changes the queries' signs instead, and one of
+    // 0, or so small, counts as 2^-100, under which all finite scores are equal, too
+    T.scale = std::max(std::fabs(d.scale) * 1.44269504088896340736f, 7.888609e-31f);
+    T.flip = d.scale < 0 ? 0x80008000u : 0u;
+    T.row_tiles = cdiv(most_rows(d), (kind == kAttnRows ? kAttnRowWaves : 1) * 16 * attn_blocks(kind, d.head_dim));
     T.split = 1;
     T.chunk = 1 << 30;
-    if (d.max_tokens > 0 && !K.by_rows) tiles += (double)d.n_seqs * d.kv_heads * T.row_tiles;
+    if (d.max_tokens > 0 && kind != kAttnRows) tiles += (double)d.n_seqs * d.kv_heads * T.row_tiles;
   }
   int64_t n_items = 0;
   for (int t = 0; t < n; ++t) {
     const st_attn_desc& d = descs[t];
     AttnDev& T = p->tenants[t];
     if (d.n_seqs == 0 || d.max_tokens == 0) continue;
-    if (!kAttnKinds[kind_of(d)].by_rows) {
+    if (kind_of(d) != kAttnRows) {
       const int steps = most_steps(d);
       int chunk;
       if (o.split_k > 0) {
@@ -200,7 +201,7 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
           for (int part = 0; part < parts; ++part)
             for (int s = 0; s < d.n_seqs; ++s)
               for (int h = 0; h < d.kv_heads; ++h)
-                p->items.push_back({(uint32_t)t, (uint32_t)s, (uint32_t)h, (uint32_t)(kAttnKinds[kind].by_rows ? parts - 1 - part : part)});
+                p->items.push_back({(uint32_t)t, (uint32_t)s, (uint32_t)h, (uint32_t)(kind == kAttnRows ? parts - 1 - part : part)});
         }
         if ((int64_t)p->items.size() > begin) p->runs.push_back({dtype, dim, kind, begin, (int64_t)p->items.size() - begin});
       }

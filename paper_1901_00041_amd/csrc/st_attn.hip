@@ -91,12 +91,13 @@ struct Attend {
   // Weights are 2^(score - m) with m lagging behind the true maximum by at most kLag; in fp16 they are moved up to the end of the type's
   // range, so that a weight has all its bits down to 2^-25 of the largest.
   static constexpr float kLag = DT == ST_DT_BF16 ? 8.f : 5.f, kUp = DT == ST_DT_BF16 ? 0.f : 10.f;
+  static constexpr float kNothing = -3.0e38f;
   static constexpr uint32_t kOnes = DT == ST_DT_BF16 ? 0x3f803f80u : 0x3c003c00u;
   typedef Mma<DT, 16> Op;
 
   u32x4 q[R][KW];
   f32x4 acc[NE][R], sum[R];
-  float m[R];              // reference, less kUp; -inf: the row has seen no token yet
+  float m[R];              // reference, less kUp; kNothing: the row has seen no token yet
   int lo[R], hi[R];        // tokens that the lane's rows see
 
   struct Raw {
@@ -110,7 +111,7 @@ struct Attend {
       constexpr int r = decltype(J)::value;
       static_for<NE>([&](auto E) { acc[decltype(E)::value][r] = f32x4{0.f, 0.f, 0.f, 0.f}; });
       sum[r] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m[r] = -__builtin_inff();
+      m[r] = kNothing;
     });
   }
   // rows [row0, row0 + 16 R) of the sequence's new tokens x heads of a group: row = token * group + head
@@ -123,7 +124,7 @@ struct Attend {
       const uint16_t* p = (const uint16_t*)T.q + (int64_t)(S.first + (real ? j : 0)) * T.ldq + (int64_t)(head * T.group + (real ? h : 0)) * D + g * (D / 4);
       static_for<KW>([&](auto B) {
         constexpr int b = decltype(B)::value;
-        q[r][b] = real ? *(const u32x4_any*)(p + 8 * b) : u32x4{0u, 0u, 0u, 0u};
+        q[r][b] = real ? *(const u32x4_any*)(p + 8 * b) ^ T.flip : u32x4{0u, 0u, 0u, 0u};
       });
       const int pos = S.before + j;
       hi[r] = !real ? -1 : T.causal ? pos : S.length - 1;
@@ -161,9 +162,53 @@ struct Attend {
     });
   }
 
-  // Tokens [32 s, 32 s + 32).  MASK: some row does not see some of them.
-  template <bool MASK>
-  __device__ __forceinline__ void step(const Raw& raw, int s, int length, float scale, int lane) {
+  // The weights of 32 tokens from t0 on, as operand B of the values' MFMAs, and their sums.  mask: some row does not see some of them; bit b
+  // of bad: nobody sees block b.
+  __device__ __forceinline__ void weigh(f32x4 (&score)[2][R], u32x4 (&p)[R], int t0, bool mask, int bad, float scale, int lane) {
+    const int g = lane >> 4;
+    if (mask) {
+      static_for<R>([&](auto J) {
+        constexpr int r = decltype(J)::value;
+        static_for<8>([&](auto X) {
+          constexpr int x = decltype(X)::value;
+          const int t = t0 + (x / 4) * 16 + 4 * g + x % 4;
+          const bool seen = (t <= hi[r]) & (t >= lo[r]) & !((bad >> (x / 4)) & 1);
+          score[x / 4][r][x % 4] = seen ? score[x / 4][r][x % 4] : -__builtin_inff();
+        });
+      });
+    }
+    float y[R][8];
+    bool above = false;
+    static_for<R>([&](auto J) {
+      constexpr int r = decltype(J)::value;
+      static_for<8>([&](auto X) { y[r][decltype(X)::value] = __builtin_fmaf(score[decltype(X)::value / 4][r][decltype(X)::value % 4], scale, -m[r]); });
+      const float top = fmaxf(fmaxf(fmaxf(y[r][0], y[r][1]), fmaxf(y[r][2], y[r][3])), fmaxf(fmaxf(y[r][4], y[r][5]), fmaxf(y[r][6], y[r][7])));
+      above |= top > kLag + kUp;
+    });
+    if (__any(above)) {
+      static_for<R>([&](auto J) {
+        constexpr int r = decltype(J)::value;
+        float top = -__builtin_inff();
+        static_for<8>([&](auto X) { top = fmaxf(top, score[decltype(X)::value / 4][r][decltype(X)::value % 4] * scale); });
+        const float next = fmaxf(m[r], max_of_row(top) - kUp), down = __builtin_amdgcn_exp2f(m[r] - next);
+        m[r] = next;
+        static_for<8>([&](auto X) { y[r][decltype(X)::value] = __builtin_fmaf(score[decltype(X)::value / 4][r][decltype(X)::value % 4], scale, -next); });
+        static_for<NE>([&](auto E) { acc[decltype(E)::value][r] *= down; });
+        sum[r] *= down;
+      });
+    }
+    static_for<R>([&](auto J) {
+      constexpr int r = decltype(J)::value;
+      static_for<4>([&](auto X) {
+        constexpr int x = decltype(X)::value;
+        p[r][x] = pack_pair<DT>(__builtin_amdgcn_exp2f(y[r][2 * x]), __builtin_amdgcn_exp2f(y[r][2 * x + 1]));
+      });
+      sum[r] = Op::run(u32x4{kOnes, kOnes, kOnes, kOnes}, p[r], sum[r]);
+    });
+  }
+
+  // Tokens [32 s, 32 s + 32).  mask: some row does not see some of them.
+  __device__ __forceinline__ void step(const Raw& raw, int s, int length, float scale, int lane, bool mask) {
     const int g = lane >> 4;
     f32x4 score[2][R];
     static_for<2>([&](auto B) {
@@ -177,59 +222,20 @@ struct Attend {
         static_for<R>([&](auto J) { score[b][decltype(J)::value] = Op::run(a, q[decltype(J)::value][w], score[b][decltype(J)::value]); });
       });
     });
-    float y[R][8];
-    bool above = false;
-    static_for<R>([&](auto J) {
-      constexpr int r = decltype(J)::value;
-      static_for<8>([&](auto X) {
-        constexpr int x = decltype(X)::value;
-        y[r][x] = __builtin_fmaf(score[x / 4][r][x % 4], scale, -m[r]);
-        if constexpr (MASK) {
-          const int t = s * kAttnStep + (x / 4) * 16 + 4 * g + x % 4;
-          const bool seen = (t <= hi[r]) & (t >= lo[r]) & !((raw.bad >> (x / 4)) & 1);
-          y[r][x] = seen ? y[r][x] : -__builtin_inff();
-        }
-      });
-      const float top = fmaxf(fmaxf(fmaxf(y[r][0], y[r][1]), fmaxf(y[r][2], y[r][3])), fmaxf(fmaxf(y[r][4], y[r][5]), fmaxf(y[r][6], y[r][7])));
-      above |= top > kLag + kUp;
-    });
-    if (__any(above)) {
-      static_for<R>([&](auto J) {
-        constexpr int r = decltype(J)::value;
-        float x8[8], top = -__builtin_inff();
-        static_for<8>([&](auto X) {
-          constexpr int x = decltype(X)::value;
-          x8[x] = score[x / 4][r][x % 4] * scale;
-          if constexpr (MASK) x8[x] = y[r][x] == -__builtin_inff() ? y[r][x] : x8[x];
-          top = fmaxf(top, x8[x]);
-        });
-        top = max_of_row(top) - kUp;
-        const float next = fmaxf(m[r], top), base = next == -__builtin_inff() ? 0.f : next;
-        const float down = __builtin_amdgcn_exp2f(m[r] - base);
-        m[r] = next;
-        static_for<8>([&](auto X) { y[r][decltype(X)::value] = x8[decltype(X)::value] - base; });
-        static_for<NE>([&](auto E) { acc[decltype(E)::value][r] *= down; });
-        sum[r] *= down;
-      });
-    }
     u32x4 p[R];
-    static_for<R>([&](auto J) {
-      constexpr int r = decltype(J)::value;
-      static_for<4>([&](auto X) {
-        constexpr int x = decltype(X)::value;
-        p[r][x] = pack_pair<DT>(__builtin_amdgcn_exp2f(y[r][2 * x]), __builtin_amdgcn_exp2f(y[r][2 * x + 1]));
-      });
-      sum[r] = Op::run(u32x4{kOnes, kOnes, kOnes, kOnes}, p[r], sum[r]);
-    });
+    weigh(score, p, s * kAttnStep, mask, raw.bad, scale, lane);
     float vsc[8];
     static_for<8>([&](auto X) {
       constexpr int x = decltype(X)::value;
       vsc[x] = value_scale<DT>((raw.vs[x / 4] >> (8 * (x % 4))) & 255u);
-      if constexpr (MASK) {                // what lies behind the sequence's end, or on no page, may be anything
+    });
+    if (mask) {                // what lies behind the sequence's end, or on no page, may be anything
+      static_for<8>([&](auto X) {
+        constexpr int x = decltype(X)::value;
         const int t = s * kAttnStep + (x / 4) * 16 + 4 * g + x % 4;
         vsc[x] = (t < length) & !((raw.bad >> (x / 4)) & 1) ? vsc[x] : 1.f;
-      }
-    });
+      });
+    }
     // two elements of the group at a time: byte e2 of a token's part of the group
     static_for<NE / 2>([&](auto E2) {
       constexpr int e2 = decltype(E2)::value;
@@ -257,11 +263,10 @@ struct Attend {
     const int final_step = end - 1;
     auto held = [&](int s) { return s < final_step ? s : final_step; };      // what is fetched ahead stays inside
     int bad = 0;
-    auto compute = [&](const Raw& raw, int s) {
+    auto compute = [&](const Raw& raw, int s) __attribute__((always_inline)) {
       bad |= raw.bad;
       const int t = s * kAttnStep;
-      if (t >= all_lo && t + kAttnStep - 1 <= all_hi && raw.bad == 0) step<false>(raw, s, length, scale, lane);
-      else step<true>(raw, s, length, scale, lane);
+      step(raw, s, length, scale, lane, !(t >= all_lo && t + kAttnStep - 1 <= all_hi && raw.bad == 0));
     };
     Raw r0, r1;
     fetch(T, r0, head, begin, last, look_up(T, seq, begin, last), lane);
@@ -301,22 +306,160 @@ __device__ __forceinline__ void store_out(ConstAttn& T, const Seq& S, int head, 
 }
 
 // ---- each wavefront its own rows ----------------------------------------------------------------------------------------
+// The wavefronts of a workgroup go through the same tokens, TT at a time.  Widening elements is most of what a step costs besides the
+// softmax, so each wavefront widens a part of the next tile into LDS, in operand order (fragment f, lane l at 16 bytes (64 f + l)),
+// while all compute on the present one: two buffers, one barrier a tile.
 template <int DT, int D, int R>
-__global__ __launch_bounds__(kAttnRowWaves * 64) void st_attn_rows_kernel(const AttnDev* table, const AttnItem* items) {
+__global__ __launch_bounds__(kAttnRowWaves * 64, D == 256 ? 1 : 2) void st_attn_rows_kernel(const AttnDev* table, const AttnItem* items) {
+  typedef Attend<DT, D, R> A;
+  constexpr int W = kAttnRowWaves, TT = D == 256 ? 32 : 64, BLOCKS = TT / 16, KW = A::KW, NE = A::NE;
+  constexpr int KF = BLOCKS * KW, VF = TT / 32 * NE;                    // fragments of a tile's keys and values
+  constexpr int KWAVE = KF / W, VWAVE = VF / W;                         // ... that a wavefront makes: of one block, of one pair of blocks
+  constexpr int KSHARE = W / BLOCKS > 0 ? W / BLOCKS : 1, VSHARE = W / (TT / 32);      // wavefronts to a block, to a pair
+  static_assert(KWAVE * KSHARE == KW && VWAVE * VSHARE == NE, "whole fragments");
+  __shared__ __align__(16) u32x4 frags[2][KF + VF][64];
+  __shared__ int hidden[2][BLOCKS];
   const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
   ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
   const int seq = (int)ci.seq, head = (int)ci.head;
-  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   const Seq S = sequence(T, seq);
-  const int rows = S.n * T.group, row0 = ((int)ci.part * kAttnRowWaves + wave) * 16 * R;
-  if (row0 >= rows) return;
+  const int rows = S.n * T.group, block0 = (int)ci.part * W * 16 * R, row0 = block0 + wave * 16 * R;
+  if (block0 >= rows) return;
+  const int block1 = block0 + W * 16 * R < rows ? block0 + W * 16 * R : rows;
   const int row1 = row0 + 16 * R < rows ? row0 + 16 * R : rows;
-  const Seen see = seen_by(T, S, row0, row1);
-  Attend<DT, D, R> a;
+  const Seen all = seen_by(T, S, block0, block1);
+  Seen see = seen_by(T, S, row0 < rows ? row0 : block0, row0 < rows ? row1 : block1);
+  if (row0 >= rows) see.hi = -1;                                         // helps widening, has nothing to compute
+  A a;
   a.clear();
   a.load_rows(T, S, head, row0, lane);
-  if (see.hi >= see.lo) a.template run<1>(T, seq, head, S.length, see.lo / kAttnStep, see.hi / kAttnStep + 1, see.hi, see.all_lo, see.all_hi, lane);
-  const int i = lane & 15, g = lane >> 4;
+  const int n0 = all.lo / TT, n1 = all.hi >= all.lo ? all.hi / TT + 1 : n0;
+  const int kb = wave / KSHARE, kq = wave % KSHARE, vu = wave / VSHARE, vq = wave % VSHARE;
+
+  // the wavefront's part of a tile as it lies in the cache
+  constexpr int VD = D == 64 ? 2 : 4;          // dwords with four tokens' elements
+  struct Raw { uint32_t k[KWAVE], v[2][VD], ks, vs[2]; int kpage, vpage[2]; };
+  struct Pages { int k, v[2]; };
+  auto place = [&](int n, int b) { return n * TT + b * 16; };
+  auto look_up = [&](int n) {
+    auto page = [&](int t) { return t <= all.hi ? page_of(T, seq, t) : -1; };
+    return Pages{page(place(n, kb)), {page(place(n, 2 * vu)), page(place(n, 2 * vu + 1))}};
+  };
+  auto fetch = [&](Raw& raw, int n, const Pages& pages) __attribute__((always_inline)) {
+    raw.kpage = pages.k;
+    {
+      const char* at = block_of(T, pages.k < 0 ? 0 : pages.k, head, place(n, kb), A::kBlock);
+      const char* kp = at + (uint32_t)(i * (D / 2) + g * (D / 8) + kq * KWAVE * 4);
+      if constexpr (KWAVE == 2) {
+        const u32x2 w = *(const u32x2*)kp;
+        raw.k[0] = w[0], raw.k[1] = w[1];
+      } else {
+        const u32x4 w = *(const u32x4*)kp;
+        static_for<4>([&](auto X) { raw.k[decltype(X)::value] = w[decltype(X)::value]; });
+      }
+      raw.ks = *(const uint8_t*)(at + (uint32_t)(16 * D + i * (D / 32) + (D == 64 ? g / 2 : D == 128 ? g : 2 * g + kq)));
+    }
+    static_for<2>([&](auto B) {
+      constexpr int b = decltype(B)::value;
+      raw.vpage[b] = pages.v[b];
+      const char* at = block_of(T, pages.v[b] < 0 ? 0 : pages.v[b], head, place(n, 2 * vu + b), A::kBlock);
+      const char* vp = at + (uint32_t)(8 * D + (i * 16 + 4 * g) * (D / 32));
+      if constexpr (D == 64) {
+        const u32x2 w = *(const u32x2*)vp;
+        raw.v[b][0] = w[0], raw.v[b][1] = w[1];
+      } else if constexpr (D == 128) {
+        const u32x4 w = *(const u32x4*)vp;
+        static_for<4>([&](auto X) { raw.v[b][decltype(X)::value] = w[decltype(X)::value]; });
+      } else {
+        static_for<4>([&](auto X) { raw.v[b][decltype(X)::value] = *(const uint32_t*)(vp + 8 * decltype(X)::value + vq / 2 * 4); });
+      }
+      raw.vs[b] = *(const uint32_t*)(at + (uint32_t)(16 * D + D / 2 + (D == 64 ? i / 8 : D == 128 ? i / 4 : i / 2) * 16 + 4 * g));
+    });
+  };
+  auto widen_tile = [&](const Raw& raw, int n, int buf) __attribute__((always_inline)) {
+    const float ksc = key_scale<DT>(raw.ks);
+    static_for<KWAVE>([&](auto F) {
+      constexpr int f = decltype(F)::value;
+      const uint32_t c = raw.k[f];
+      frags[buf][kb * KW + kq * KWAVE + f][lane] = u32x4{widen<DT, 0>(c, ksc), widen<DT, 1>(c, ksc), widen<DT, 2>(c, ksc), widen<DT, 3>(c, ksc)};
+    });
+    if (lane == 0 && kq == 0) hidden[buf][kb] = raw.kpage < 0;
+    float vsc[8];
+    static_for<8>([&](auto X) {          // what lies behind the sequence's end, or on no page, may be anything
+      constexpr int x = decltype(X)::value;
+      const int t = place(n, 2 * vu) + x / 4 * 16 + 4 * g + x % 4;
+      vsc[x] = (t < S.length) & (raw.vpage[x / 4] >= 0) ? value_scale<DT>((raw.vs[x / 4] >> (8 * (x % 4))) & 255u) : 1.f;
+    });
+    // elements 2 e2, 2 e2 + 1 of the groups, for the wavefront's e2; token t's byte of them
+    static_for<VWAVE / 2>([&](auto E) {
+      constexpr int e = decltype(E)::value;
+      auto byte = [&](auto B, auto X, float f) __attribute__((always_inline)) {
+        constexpr int b = decltype(B)::value, t = decltype(X)::value;
+        if constexpr (D == 64) return widen<DT, t % 2 * 2>(raw.v[b][t / 2] >> (8 * vq), f);
+        else return widen<DT, e>(raw.v[b][t] >> (16 * (vq % 2)), f);
+      };
+      u32x4 a0, a1;
+      static_for<4>([&](auto X) {
+        constexpr int x = decltype(X)::value, b = x / 2, t = 2 * (x % 2);
+        const std::integral_constant<int, b> bb{};
+        const uint32_t c0 = byte(bb, std::integral_constant<int, t>{}, vsc[4 * b + t]), c1 = byte(bb, std::integral_constant<int, t + 1>{}, vsc[4 * b + t + 1]);
+        a0[x] = __builtin_amdgcn_perm(c1, c0, 0x05040100u);
+        a1[x] = __builtin_amdgcn_perm(c1, c0, 0x07060302u);
+      });
+      u32x4* to = &frags[buf][KF + vu * NE + vq * VWAVE + 2 * e][lane];
+      to[0] = a0;
+      to[64] = a1;
+    });
+  };
+  const float scale = T.scale;
+  auto sub_step = [&](bool mask, int buf, int u, int t0, int bad) __attribute__((always_inline)) {
+    f32x4 score[2][R];
+    static_for<2>([&](auto B) {
+      static_for<R>([&](auto J) { score[decltype(B)::value][decltype(J)::value] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+      static_for<KW>([&](auto Q) {
+        constexpr int b = decltype(B)::value, w = decltype(Q)::value;
+        if constexpr (w % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+        const u32x4 f = frags[buf][(2 * u + b) * KW + w][lane];
+        static_for<R>([&](auto J) { score[b][decltype(J)::value] = A::Op::run(f, a.q[decltype(J)::value][w], score[b][decltype(J)::value]); });
+      });
+    });
+    u32x4 p[R];
+    a.weigh(score, p, t0, mask, bad, scale, lane);
+    static_for<NE>([&](auto E) {
+      constexpr int e = decltype(E)::value;
+      if constexpr (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+      const u32x4 f = frags[buf][KF + u * NE + e][lane];
+      static_for<R>([&](auto J) { a.acc[e][decltype(J)::value] = A::Op::run(f, p[decltype(J)::value], a.acc[e][decltype(J)::value]); });
+    });
+  };
+  int bad_pages = 0;
+  if (n0 < n1) {
+    auto held = [&](int n) { return n < n1 - 1 ? n : n1 - 1; };      // what is fetched ahead stays inside
+    Raw raw;
+    fetch(raw, n0, look_up(n0));
+    widen_tile(raw, n0, 0);
+    fetch(raw, held(n0 + 1), look_up(held(n0 + 1)));
+    Pages next = look_up(held(n0 + 2));
+    __syncthreads();
+    for (int n = n0; n < n1; ++n) {
+      const int buf = (n - n0) & 1;
+      if (n + 1 < n1) widen_tile(raw, n + 1, buf ^ 1);
+      fetch(raw, held(n + 2), next);
+      next = look_up(held(n + 3));
+      if (n * TT <= see.hi && n * TT + TT - 1 >= see.lo) {
+#pragma unroll 1
+        for (int u = 0; u < TT / 32; ++u) {
+          const int t0 = n * TT + 32 * u, bad = __builtin_amdgcn_readfirstlane(hidden[buf][2 * u] | hidden[buf][2 * u + 1] << 1);
+          if (t0 + 16 <= all.hi) bad_pages |= bad;
+          else if (t0 <= all.hi) bad_pages |= bad & 1;
+          if (t0 <= see.hi && t0 + 31 >= see.lo) sub_step(!(t0 >= see.all_lo && t0 + 31 <= see.all_hi && bad == 0), buf, u, t0, bad);
+        }
+      }
+      __syncthreads();
+    }
+  }
+  if (bad_pages && lane == 0) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_PAGE);
   static_for<R>([&](auto J) {
     constexpr int r = decltype(J)::value;
     const int row = row0 + r * 16 + i;
@@ -372,10 +515,10 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64) void st_attn_tokens_kernel(co
   float ref[R];
   static_for<R>([&](auto J) {
     constexpr int r = decltype(J)::value;
-    float top = -__builtin_inff();
+    float top = a.m[r];
     for (int w = 0; w < W; ++w) top = fmaxf(top, wave_m[w][r * 16 + i]);
     ref[r] = top;
-    const float down = a.m[r] == -__builtin_inff() && a.sum[r][0] == 0.f ? 0.f : __builtin_amdgcn_exp2f(a.m[r] - top);
+    const float down = __builtin_amdgcn_exp2f(a.m[r] - top);
     static_for<D / 16>([&](auto E) { a.acc[decltype(E)::value][r] *= down; });
     if (g == 0) wave_l[wave][r * 16 + i] = a.sum[r][0] * down;
   });
@@ -442,7 +585,7 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64) void st_attn_tokens_kernel(co
   __syncthreads();
   if (flag == 0u) return;
   if (tid < ROWS) {
-    float top = -__builtin_inff(), total = 0.f;
+    float top = Attend<DT, D, R>::kNothing, total = 0.f;
     for (int s = 0; s < active; ++s) {
       const float ms = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rstat, (s * 2 * ROWS + tid) * 4, 0, kAuxDeviceCoherent));
       weight[s][tid] = ms;
@@ -450,7 +593,7 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64) void st_attn_tokens_kernel(co
     }
     for (int s = 0; s < active; ++s) {
       const float l = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rstat, (s * 2 * ROWS + ROWS + tid) * 4, 0, kAuxDeviceCoherent));
-      const float w = weight[s][tid] == -__builtin_inff() && l == 0.f ? 0.f : __builtin_amdgcn_exp2f(weight[s][tid] - top);
+      const float w = __builtin_amdgcn_exp2f(weight[s][tid] - top);
       weight[s][tid] = w;
       total += w * l;
     }
@@ -579,11 +722,9 @@ __global__ __launch_bounds__(256) void st_attn_move_kernel(const AttnDev* table,
 template <int DT, int D>
 static hipError_t launch_kind(int kind, unsigned blocks, void* stream, const AttnDev* table, const AttnItem* items) {
   switch (kind) {
-    case 0: return launch(st_attn_tokens_kernel<DT, D, 1>, blocks, kAttnTokenWaves * 64, stream, table, items);
-    case 1: return launch(st_attn_tokens_kernel<DT, D, 2>, blocks, kAttnTokenWaves * 64, stream, table, items);
-    case 2: return launch(st_attn_rows_kernel<DT, D, 2>, blocks, kAttnRowWaves * 64, stream, table, items);
-    case 3:
-      if constexpr (D <= 128) return launch(st_attn_rows_kernel<DT, D, 4>, blocks, kAttnRowWaves * 64, stream, table, items);
+    case kAttnTokens1: return launch(st_attn_tokens_kernel<DT, D, attn_blocks(kAttnTokens1, D)>, blocks, kAttnTokenWaves * 64, stream, table, items);
+    case kAttnTokens2: return launch(st_attn_tokens_kernel<DT, D, attn_blocks(kAttnTokens2, D)>, blocks, kAttnTokenWaves * 64, stream, table, items);
+    case kAttnRows: return launch(st_attn_rows_kernel<DT, D, attn_blocks(kAttnRows, D)>, blocks, kAttnRowWaves * 64, stream, table, items);
   }
   return hipErrorInvalidValue;
 }

@@ -58,9 +58,9 @@ constexpr int kAttnBlock = 16;           // tokens per cache block
 constexpr int kAttnStep = 32;            // tokens per step of a wavefront
 constexpr int kAttnTokenWaves = 8, kAttnRowWaves = 4;
 constexpr int kAttnMaxSplit = 64;
-struct AttnKind { bool by_rows; int R; };
-constexpr AttnKind kAttnKinds[] = {{false, 1}, {false, 2}, {true, 2}, {true, 4}};
-constexpr int kNumAttnKinds = (int)(sizeof(kAttnKinds) / sizeof(kAttnKinds[0]));
+constexpr int kAttnTokens1 = 0, kAttnTokens2 = 1, kAttnRows = 2, kNumAttnKinds = 3;
+// R of a kind: rows are as many as the registers hold beside their queries, scores and outputs
+constexpr int attn_blocks(int kind, int dim) { return kind == kAttnTokens1 ? 1 : kind == kAttnTokens2 ? (dim == 256 ? 1 : 2) : dim == 64 ? 4 : dim == 128 ? 3 : 2; }
 
 // Bytes of a block of 16 tokens of one head, and where its parts begin.
 constexpr int attn_block_bytes(int dim) { return kAttnBlock * (dim + dim / 16); }
@@ -84,10 +84,10 @@ struct AttnDev {
   int32_t heads, kv_heads, group, n_seqs;
   int32_t max_tokens, max_new, n_pages, page_shift;
   int32_t table_pages, window, causal;
-  float scale;           // times log2(e)
+  float scale;           // its size times log2(e), above zero
   int32_t row_tiles;     // per sequence and key head
   int32_t split, chunk;  // at most `split` stretches of `chunk` steps
-  int32_t pad;
+  uint32_t flip;         // sign bits of two query elements, where scale is negative
 };
 static_assert(sizeof(AttnDev) == 208, "a multiple of 16 bytes for launch_poke");
 
