@@ -53,9 +53,9 @@ st_status validate_sizes(const st_attn_desc& d, int t) {
   const int64_t wide = (int64_t)d.heads * d.head_dim, narrow = (int64_t)d.kv_heads * d.head_dim, far = (int64_t)1 << 32;
   if (d.ldq < 0 || d.ldk < 0 || d.ldv < 0 || d.ldo < 0 || (d.ldq && d.ldq < wide) || (d.ldo && d.ldo < wide) || (d.ldk && d.ldk < narrow) || (d.ldv && d.ldv < narrow))
     return fail(ST_ERR_INVALID_ARG, "tenant %d: rows must not overlap the rows behind them", t);
-  if (d.heads > (1 << 16) || std::max(std::max(d.ldq, d.ldk), std::max(d.ldv, d.ldo)) > far || (int64_t)d.table_pages * d.page_tokens >= ((int64_t)1 << 30) ||
+  if (d.heads > (1 << 16) || page_bytes(d) >= ((int64_t)1 << 31) || std::max(std::max(d.ldq, d.ldk), std::max(d.ldv, d.ldo)) > far || (int64_t)d.table_pages * d.page_tokens >= ((int64_t)1 << 30) ||
       (int64_t)d.max_new * (d.heads / d.kv_heads) >= ((int64_t)1 << 30) || d.max_tokens >= (1 << 30) || d.n_seqs >= (1 << 24))
-    return fail(ST_ERR_UNSUPPORTED, "tenant %d: more than 2^16 heads, rows more than 2^32 elements apart, or 2^30 tokens or more", t);
+    return fail(ST_ERR_UNSUPPORTED, "tenant %d: more than 2^16 heads, a page of 2^31 bytes, rows more than 2^32 elements apart, or 2^30 tokens or more", t);
   return ST_OK;
 }
 

@@ -41,14 +41,34 @@ __device__ __forceinline__ Seq sequence(ConstAttn& T, int seq) {
   if (threadIdx.x == 0 && (f0 != a || f1 != b || length != len || n != all || all > length)) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_LENGTH);
   return {f0, n, length, length - all};
 }
-// The page of token t (t >= 0, below the table's end), or -1.
-__device__ __forceinline__ int page_of(ConstAttn& T, int seq, int t) {
-  const int page = ((ConstInt*)T.table)[(int64_t)seq * T.table_pages + (t >> T.page_shift)];
-  return (uint32_t)page < (uint32_t)T.n_pages ? page : -1;
-}
+// A stretch of a sequence's table, an entry a lane, so that looking a page up costs no trip to memory (nor a scalar load, which would
+// make every wait for LDS a wait for all of it).
+struct Table {
+  int entry, base;
+  const int32_t* row;
+  int last;               // column of the last token that is looked up
+  __device__ __forceinline__ void load(int column, int lane) {
+    base = column;
+    entry = row[column + lane < last ? column + lane : last];
+    __builtin_amdgcn_s_waitcnt(0x0f70);      // here: else every look-up waits for all loads in flight, in case this one is among them
+  }
+  __device__ __forceinline__ Table(ConstAttn& T, int seq, int first_token, int last_token, int lane) {
+    row = T.table + (int64_t)seq * T.table_pages;
+    last = last_token >> T.page_shift;
+    load(first_token >> T.page_shift, lane);
+  }
+  // the page of token t (not before those already looked up, except by a few), or -1; t may lie behind the last one
+  __device__ __forceinline__ int page(ConstAttn& T, int t, int lane) {
+    const int column = t >> T.page_shift;
+    if (column > last) return -1;
+    if ((unsigned)(column - base) >= 64u) load(column, lane);
+    const int p = __builtin_amdgcn_readlane(entry, column - base);
+    return (uint32_t)p < (uint32_t)T.n_pages ? p : -1;
+  }
+};
 __device__ __forceinline__ const char* block_of(ConstAttn& T, int page, int head, int t, int block_bytes) {
-  const int in_page = t & ((1 << T.page_shift) - 1), blocks = 1 << (T.page_shift - 4);
-  return (const char*)T.pages + (int64_t)page * T.page_bytes + ((int64_t)head * blocks + (in_page >> 4)) * block_bytes;
+  const uint32_t in_page = (uint32_t)t & ((1u << T.page_shift) - 1u), blocks = 1u << (T.page_shift - 4);
+  return (const char*)T.pages + (uint64_t)(uint32_t)page * (uint32_t)T.page_bytes + ((uint32_t)head * blocks + (in_page >> 4)) * (uint32_t)block_bytes;
 }
 
 // ---- elements and scales ----------------------------------------------------------------------------------------------
@@ -76,6 +96,9 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
   if constexpr (DT == ST_DT_BF16) return pack16<DT>(a, b);
   else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
 }
+// The larger of two values in one instruction: as a median with an infinity that the compiler does not know (fmaxf of what an MFMA left
+// costs another one per operand, which quiets NaNs).
+__device__ __forceinline__ float max_raw(float a, float b, float inf) { return __builtin_amdgcn_fmed3f(a, b, inf); }
 __device__ __forceinline__ float max_of_row(float v) {      // over the four lanes that hold a query row
   v = fmaxf(v, __shfl_xor(v, 16));
   return fmaxf(v, __shfl_xor(v, 32));
@@ -98,7 +121,7 @@ struct Attend {
   u32x4 q[R][KW];
   f32x4 acc[NE][R], sum[R];
   float m[R];              // reference, less kUp; kNothing: the row has seen no token yet
-  int lo[R], hi[R];        // tokens that the lane's rows see
+  int pos[R];              // the lane's rows' tokens; a row that there is not has queries of 0 and is not stored
 
   struct Raw {
     uint32_t k[2][KW], v[2][VW], ks[2], vs[2];
@@ -126,15 +149,14 @@ struct Attend {
         constexpr int b = decltype(B)::value;
         q[r][b] = real ? *(const u32x4_any*)(p + 8 * b) ^ T.flip : u32x4{0u, 0u, 0u, 0u};
       });
-      const int pos = S.before + j;
-      hi[r] = !real ? -1 : T.causal ? pos : S.length - 1;
-      lo[r] = T.window ? pos - T.window + 1 : 0;
+      pos[r] = T.causal ? S.before + j : S.length - 1;
     });
   }
   // the page of both blocks of step s; a block behind `last` takes the first one's
-  static __device__ __forceinline__ Pages look_up(ConstAttn& T, int seq, int s, int last) {
+  static __device__ __forceinline__ Pages look_up(ConstAttn& T, Table& table, int s, int last, int lane) {
     const int t = s * kAttnStep;
-    return {{page_of(T, seq, t), page_of(T, seq, t + 16 <= last ? t + 16 : t)}};
+    const int a = table.page(T, t, lane);
+    return {{a, t + 16 <= last ? table.page(T, t + 16, lane) : a}};
   }
   static __device__ __forceinline__ void fetch(ConstAttn& T, Raw& raw, int head, int s, int last, const Pages& pages, int lane) {
     const int i = lane & 15, g = lane >> 4;
@@ -164,35 +186,35 @@ struct Attend {
 
   // The weights of 32 tokens from t0 on, as operand B of the values' MFMAs, and their sums.  mask: some row does not see some of them; bit b
   // of bad: nobody sees block b.
-  __device__ __forceinline__ void weigh(f32x4 (&score)[2][R], u32x4 (&p)[R], int t0, bool mask, int bad, float scale, int lane) {
-    const int g = lane >> 4;
+  __device__ __forceinline__ void weigh(f32x4 (&score)[2][R], u32x4 (&p)[R], int t0, bool mask, int bad, int window, float scale, int lane) {
     if (mask) {
+      const int g = lane >> 4;
       static_for<R>([&](auto J) {
         constexpr int r = decltype(J)::value;
         static_for<8>([&](auto X) {
           constexpr int x = decltype(X)::value;
           const int t = t0 + (x / 4) * 16 + 4 * g + x % 4;
-          const bool seen = (t <= hi[r]) & (t >= lo[r]) & !((bad >> (x / 4)) & 1);
+          // without a window (0, taken as 2^32 - 1) only t <= pos counts
+          const bool seen = ((uint32_t)(pos[r] - t) <= (uint32_t)window - 1u) & (t <= pos[r]) & !((bad >> (x / 4)) & 1);
           score[x / 4][r][x % 4] = seen ? score[x / 4][r][x % 4] : -__builtin_inff();
         });
       });
     }
-    float y[R][8];
+    // the scale is above zero: a row's largest score is its largest exponent
+    float top[R], inf;
+    asm("s_mov_b32 %0, 0x7f800000" : "=s"(inf));
     bool above = false;
     static_for<R>([&](auto J) {
       constexpr int r = decltype(J)::value;
-      static_for<8>([&](auto X) { y[r][decltype(X)::value] = __builtin_fmaf(score[decltype(X)::value / 4][r][decltype(X)::value % 4], scale, -m[r]); });
-      const float top = fmaxf(fmaxf(fmaxf(y[r][0], y[r][1]), fmaxf(y[r][2], y[r][3])), fmaxf(fmaxf(y[r][4], y[r][5]), fmaxf(y[r][6], y[r][7])));
-      above |= top > kLag + kUp;
+      const f32x4 a = score[0][r], b = score[1][r];
+      top[r] = max_raw(max_raw(max_raw(a[0], a[1], inf), max_raw(a[2], a[3], inf), inf), max_raw(max_raw(b[0], b[1], inf), max_raw(b[2], b[3], inf), inf), inf);
+      above |= __builtin_fmaf(top[r], scale, -m[r]) > kLag + kUp;
     });
-    if (__any(above)) {
+    if (__builtin_expect(__any(above) != 0, 0)) {
       static_for<R>([&](auto J) {
         constexpr int r = decltype(J)::value;
-        float top = -__builtin_inff();
-        static_for<8>([&](auto X) { top = fmaxf(top, score[decltype(X)::value / 4][r][decltype(X)::value % 4] * scale); });
-        const float next = fmaxf(m[r], max_of_row(top) - kUp), down = __builtin_amdgcn_exp2f(m[r] - next);
+        const float next = fmaxf(m[r], max_of_row(top[r]) * scale - kUp), down = __builtin_amdgcn_exp2f(m[r] - next);
         m[r] = next;
-        static_for<8>([&](auto X) { y[r][decltype(X)::value] = __builtin_fmaf(score[decltype(X)::value / 4][r][decltype(X)::value % 4], scale, -next); });
         static_for<NE>([&](auto E) { acc[decltype(E)::value][r] *= down; });
         sum[r] *= down;
       });
@@ -201,14 +223,15 @@ struct Attend {
       constexpr int r = decltype(J)::value;
       static_for<4>([&](auto X) {
         constexpr int x = decltype(X)::value;
-        p[r][x] = pack_pair<DT>(__builtin_amdgcn_exp2f(y[r][2 * x]), __builtin_amdgcn_exp2f(y[r][2 * x + 1]));
+        auto weight = [&](int e) { return __builtin_amdgcn_exp2f(__builtin_fmaf(score[x / 2][r][e], scale, -m[r])); };
+        p[r][x] = pack_pair<DT>(weight(x % 2 * 2), weight(x % 2 * 2 + 1));
       });
       sum[r] = Op::run(u32x4{kOnes, kOnes, kOnes, kOnes}, p[r], sum[r]);
     });
   }
 
   // Tokens [32 s, 32 s + 32).  mask: some row does not see some of them.
-  __device__ __forceinline__ void step(const Raw& raw, int s, int length, float scale, int lane, bool mask) {
+  __device__ __forceinline__ void step(const Raw& raw, int s, int length, int window, float scale, int lane, bool mask) {
     const int g = lane >> 4;
     f32x4 score[2][R];
     static_for<2>([&](auto B) {
@@ -223,7 +246,7 @@ struct Attend {
       });
     });
     u32x4 p[R];
-    weigh(score, p, s * kAttnStep, mask, raw.bad, scale, lane);
+    weigh(score, p, s * kAttnStep, mask, raw.bad, window, scale, lane);
     float vsc[8];
     static_for<8>([&](auto X) {
       constexpr int x = decltype(X)::value;
@@ -266,18 +289,19 @@ struct Attend {
     auto compute = [&](const Raw& raw, int s) __attribute__((always_inline)) {
       bad |= raw.bad;
       const int t = s * kAttnStep;
-      step(raw, s, length, scale, lane, !(t >= all_lo && t + kAttnStep - 1 <= all_hi && raw.bad == 0));
+      step(raw, s, length, T.window, scale, lane, !(t >= all_lo && t + kAttnStep - 1 <= all_hi && raw.bad == 0));
     };
+    Table table(T, seq, begin * kAttnStep, last, lane);
     Raw r0, r1;
-    fetch(T, r0, head, begin, last, look_up(T, seq, begin, last), lane);
-    Pages next = look_up(T, seq, held(begin + STRIDE), last);
+    fetch(T, r0, head, begin, last, look_up(T, table, begin, last, lane), lane);
+    Pages next = look_up(T, table, held(begin + STRIDE), last, lane);
     for (int s = begin; s < end; s += 2 * STRIDE) {
       fetch(T, r1, head, held(s + STRIDE), last, next, lane);
-      next = look_up(T, seq, held(s + 2 * STRIDE), last);
+      next = look_up(T, table, held(s + 2 * STRIDE), last, lane);
       compute(r0, s);
       if (s + STRIDE >= end) break;
       fetch(T, r0, head, held(s + 2 * STRIDE), last, next, lane);
-      next = look_up(T, seq, held(s + 3 * STRIDE), last);
+      next = look_up(T, table, held(s + 3 * STRIDE), last, lane);
       compute(r1, s + STRIDE);
     }
     if (bad && lane == 0) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_PAGE);
@@ -306,19 +330,20 @@ __device__ __forceinline__ void store_out(ConstAttn& T, const Seq& S, int head, 
 }
 
 // ---- each wavefront its own rows ----------------------------------------------------------------------------------------
-// The wavefronts of a workgroup go through the same tokens, TT at a time.  Widening elements is most of what a step costs besides the
-// softmax, so each wavefront widens a part of the next tile into LDS, in operand order (fragment f, lane l at 16 bytes (64 f + l)),
-// while all compute on the present one: two buffers, one barrier a tile.
+// The wavefronts of a workgroup go through the same tokens, TT at a time.  Each of them widens a block of the next tile (or half of
+// one) into LDS, in operand order (fragment f, lane l at 16 bytes (64 f + l)), while all compute on the present one: two buffers, one
+// barrier a tile.  A wavefront issues a vector instruction every five to six clocks at best and its MFMAs take sixteen each, so the
+// widening is cut into pieces that are issued between MFMAs.
 template <int DT, int D, int R>
-__global__ __launch_bounds__(kAttnRowWaves * 64, D == 256 ? 1 : 2) void st_attn_rows_kernel(const AttnDev* table, const AttnItem* items) {
+__global__ __launch_bounds__(kAttnRowWaves * 64, 2) void st_attn_rows_kernel(const AttnDev* table, const AttnItem* items) {
   typedef Attend<DT, D, R> A;
   constexpr int W = kAttnRowWaves, TT = D == 256 ? 32 : 64, BLOCKS = TT / 16, KW = A::KW, NE = A::NE;
-  constexpr int KF = BLOCKS * KW, VF = TT / 32 * NE;                    // fragments of a tile's keys and values
-  constexpr int KWAVE = KF / W, VWAVE = VF / W;                         // ... that a wavefront makes: of one block, of one pair of blocks
-  constexpr int KSHARE = W / BLOCKS > 0 ? W / BLOCKS : 1, VSHARE = W / (TT / 32);      // wavefronts to a block, to a pair
-  static_assert(KWAVE * KSHARE == KW && VWAVE * VSHARE == NE, "whole fragments");
+  constexpr int SHARE = W / BLOCKS;                                     // wavefronts to a block
+  constexpr int KWAVE = KW / SHARE, VWAVE = NE / SHARE;                 // fragments that a wavefront makes of its block's keys and values
+  constexpr int KF = BLOCKS * KW, VF = TT / 32 * NE;                    // fragments of a tile
+  static_assert(W % BLOCKS == 0 && KW % SHARE == 0 && (KWAVE == 2 || KWAVE == 4), "whole fragments");
   __shared__ __align__(16) u32x4 frags[2][KF + VF][64];
-  __shared__ int hidden[2][BLOCKS];
+  __shared__ __align__(16) int hidden[2][BLOCKS];
   const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
   ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
   const int seq = (int)ci.seq, head = (int)ci.head;
@@ -335,127 +360,123 @@ __global__ __launch_bounds__(kAttnRowWaves * 64, D == 256 ? 1 : 2) void st_attn_
   a.clear();
   a.load_rows(T, S, head, row0, lane);
   const int n0 = all.lo / TT, n1 = all.hi >= all.lo ? all.hi / TT + 1 : n0;
-  const int kb = wave / KSHARE, kq = wave % KSHARE, vu = wave / VSHARE, vq = wave % VSHARE;
+  const int kb = wave / SHARE, part = wave % SHARE;                     // the wavefront's block of a tile, and its part of it
 
-  // the wavefront's part of a tile as it lies in the cache
-  constexpr int VD = D == 64 ? 2 : 4;          // dwords with four tokens' elements
-  struct Raw { uint32_t k[KWAVE], v[2][VD], ks, vs[2]; int kpage, vpage[2]; };
-  struct Pages { int k, v[2]; };
-  auto place = [&](int n, int b) { return n * TT + b * 16; };
-  auto look_up = [&](int n) {
-    auto page = [&](int t) { return t <= all.hi ? page_of(T, seq, t) : -1; };
-    return Pages{page(place(n, kb)), {page(place(n, 2 * vu)), page(place(n, 2 * vu + 1))}};
+  struct Raw { uint32_t k[KWAVE], v[4], ks, vs; int page; };            // the part as it lies in the cache; v: a word per token (D = 64: per two)
+  Raw raw;
+  Table pages_of(T, seq, n0 < n1 ? n0 * TT : 0, n0 < n1 ? all.hi : 0, lane);
+  const uint32_t k_at = (uint32_t)(i * (D / 2) + g * (D / 8) + part * KWAVE * 4), v_at = (uint32_t)(8 * D + (i * 16 + 4 * g) * (D / 32) + part * 4);
+  const uint32_t ks_at = (uint32_t)(16 * D + i * (D / 32) + (D == 64 ? g / 2 : D == 128 ? g : 2 * g + part));
+  const uint32_t vs_at = (uint32_t)(16 * D + D / 2 + (D == 64 ? i / 8 : D == 128 ? i / 4 : i / 2) * 16 + 4 * g);
+  auto look_up = [&](int n) __attribute__((always_inline)) {
+    const int t = n * TT + kb * 16;
+    return t <= all.hi ? pages_of.page(T, t, lane) : -1;
   };
-  auto fetch = [&](Raw& raw, int n, const Pages& pages) __attribute__((always_inline)) {
-    raw.kpage = pages.k;
-    {
-      const char* at = block_of(T, pages.k < 0 ? 0 : pages.k, head, place(n, kb), A::kBlock);
-      const char* kp = at + (uint32_t)(i * (D / 2) + g * (D / 8) + kq * KWAVE * 4);
-      if constexpr (KWAVE == 2) {
-        const u32x2 w = *(const u32x2*)kp;
-        raw.k[0] = w[0], raw.k[1] = w[1];
+  auto fetch = [&](int n, int page) __attribute__((always_inline)) {
+    const int t = n * TT + kb * 16;
+    raw.page = page;
+    const char* at = block_of(T, raw.page < 0 ? 0 : raw.page, head, t, A::kBlock);
+    if constexpr (KWAVE == 2) {
+      const u32x2 w = *(const u32x2*)(at + k_at), c = *(const u32x2*)(at + v_at);
+      raw.k[0] = w[0], raw.k[1] = w[1], raw.v[0] = c[0], raw.v[1] = c[1];
+    } else {
+      const u32x4 w = *(const u32x4*)(at + k_at);
+      static_for<4>([&](auto X) { raw.k[decltype(X)::value] = w[decltype(X)::value]; });
+      if constexpr (SHARE == 1) {
+        const u32x4 c = *(const u32x4*)(at + v_at);
+        static_for<4>([&](auto X) { raw.v[decltype(X)::value] = c[decltype(X)::value]; });
       } else {
-        const u32x4 w = *(const u32x4*)kp;
-        static_for<4>([&](auto X) { raw.k[decltype(X)::value] = w[decltype(X)::value]; });
+        static_for<4>([&](auto X) { raw.v[decltype(X)::value] = *(const uint32_t*)(at + v_at + 8 * decltype(X)::value); });
       }
-      raw.ks = *(const uint8_t*)(at + (uint32_t)(16 * D + i * (D / 32) + (D == 64 ? g / 2 : D == 128 ? g : 2 * g + kq)));
     }
-    static_for<2>([&](auto B) {
-      constexpr int b = decltype(B)::value;
-      raw.vpage[b] = pages.v[b];
-      const char* at = block_of(T, pages.v[b] < 0 ? 0 : pages.v[b], head, place(n, 2 * vu + b), A::kBlock);
-      const char* vp = at + (uint32_t)(8 * D + (i * 16 + 4 * g) * (D / 32));
-      if constexpr (D == 64) {
-        const u32x2 w = *(const u32x2*)vp;
-        raw.v[b][0] = w[0], raw.v[b][1] = w[1];
-      } else if constexpr (D == 128) {
-        const u32x4 w = *(const u32x4*)vp;
-        static_for<4>([&](auto X) { raw.v[b][decltype(X)::value] = w[decltype(X)::value]; });
-      } else {
-        static_for<4>([&](auto X) { raw.v[b][decltype(X)::value] = *(const uint32_t*)(vp + 8 * decltype(X)::value + vq / 2 * 4); });
-      }
-      raw.vs[b] = *(const uint32_t*)(at + (uint32_t)(16 * D + D / 2 + (D == 64 ? i / 8 : D == 128 ? i / 4 : i / 2) * 16 + 4 * g));
-    });
+    raw.ks = *(const uint8_t*)(at + ks_at);
+    raw.vs = *(const uint32_t*)(at + vs_at);
   };
-  auto widen_tile = [&](const Raw& raw, int n, int buf) __attribute__((always_inline)) {
-    const float ksc = key_scale<DT>(raw.ks);
-    static_for<KWAVE>([&](auto F) {
-      constexpr int f = decltype(F)::value;
+  // the pieces of making tile n in buffer buf from what was fetched, and of fetching tile n + 1 (held inside the range) after it
+  constexpr int PIECES = 2 + KWAVE + VWAVE / 2;
+  float ksc, vsc[4];
+  int next_page = -1;
+  auto piece = [&](auto P, int n, int buf) __attribute__((always_inline)) {
+    constexpr int p = decltype(P)::value;
+    if constexpr (p == 0) {
+      ksc = key_scale<DT>(raw.ks);
+      static_for<4>([&](auto X) { vsc[decltype(X)::value] = value_scale<DT>((raw.vs >> (8 * decltype(X)::value)) & 255u); });
+      // what lies behind the sequence's end, or on no page, may be anything: it takes a scale of 1
+      const int real = raw.page < 0 ? 0 : S.length - (n * TT + kb * 16 + 4 * g);
+      static_for<4>([&](auto X) { vsc[decltype(X)::value] = decltype(X)::value < real ? vsc[decltype(X)::value] : 1.f; });
+      hidden[buf][kb] = raw.page < 0;
+    } else if constexpr (p <= KWAVE) {
+      constexpr int f = p - 1;
       const uint32_t c = raw.k[f];
-      frags[buf][kb * KW + kq * KWAVE + f][lane] = u32x4{widen<DT, 0>(c, ksc), widen<DT, 1>(c, ksc), widen<DT, 2>(c, ksc), widen<DT, 3>(c, ksc)};
-    });
-    if (lane == 0 && kq == 0) hidden[buf][kb] = raw.kpage < 0;
-    float vsc[8];
-    static_for<8>([&](auto X) {          // what lies behind the sequence's end, or on no page, may be anything
-      constexpr int x = decltype(X)::value;
-      const int t = place(n, 2 * vu) + x / 4 * 16 + 4 * g + x % 4;
-      vsc[x] = (t < S.length) & (raw.vpage[x / 4] >= 0) ? value_scale<DT>((raw.vs[x / 4] >> (8 * (x % 4))) & 255u) : 1.f;
-    });
-    // elements 2 e2, 2 e2 + 1 of the groups, for the wavefront's e2; token t's byte of them
-    static_for<VWAVE / 2>([&](auto E) {
-      constexpr int e = decltype(E)::value;
-      auto byte = [&](auto B, auto X, float f) __attribute__((always_inline)) {
-        constexpr int b = decltype(B)::value, t = decltype(X)::value;
-        if constexpr (D == 64) return widen<DT, t % 2 * 2>(raw.v[b][t / 2] >> (8 * vq), f);
-        else return widen<DT, e>(raw.v[b][t] >> (16 * (vq % 2)), f);
-      };
-      u32x4 a0, a1;
+      frags[buf][kb * KW + part * KWAVE + f][lane] = u32x4{widen<DT, 0>(c, ksc), widen<DT, 1>(c, ksc), widen<DT, 2>(c, ksc), widen<DT, 3>(c, ksc)};
+    } else if constexpr (p <= KWAVE + VWAVE / 2) {
+      constexpr int e2 = p - 1 - KWAVE;             // elements 2 e2, 2 e2 + 1 of the part's groups, for the lane's four tokens
+      uint32_t c[4];
       static_for<4>([&](auto X) {
-        constexpr int x = decltype(X)::value, b = x / 2, t = 2 * (x % 2);
-        const std::integral_constant<int, b> bb{};
-        const uint32_t c0 = byte(bb, std::integral_constant<int, t>{}, vsc[4 * b + t]), c1 = byte(bb, std::integral_constant<int, t + 1>{}, vsc[4 * b + t + 1]);
-        a0[x] = __builtin_amdgcn_perm(c1, c0, 0x05040100u);
-        a1[x] = __builtin_amdgcn_perm(c1, c0, 0x07060302u);
+        constexpr int t = decltype(X)::value;
+        if constexpr (D == 64) c[t] = widen<DT, t % 2 * 2 + e2>(raw.v[t / 2], vsc[t]);
+        else c[t] = widen<DT, e2>(raw.v[t], vsc[t]);
       });
-      u32x4* to = &frags[buf][KF + vu * NE + vq * VWAVE + 2 * e][lane];
-      to[0] = a0;
-      to[64] = a1;
-    });
+      u32x2* to = (u32x2*)&frags[buf][KF + kb / 2 * NE + part * VWAVE + 2 * e2][lane] + kb % 2;
+      to[0] = u32x2{__builtin_amdgcn_perm(c[1], c[0], 0x05040100u), __builtin_amdgcn_perm(c[3], c[2], 0x05040100u)};
+      to[128] = u32x2{__builtin_amdgcn_perm(c[1], c[0], 0x07060302u), __builtin_amdgcn_perm(c[3], c[2], 0x07060302u)};
+    } else {
+      fetch(n + 1 < n1 ? n + 1 : n1 - 1, next_page);
+    }
   };
   const float scale = T.scale;
-  auto sub_step = [&](bool mask, int buf, int u, int t0, int bad) __attribute__((always_inline)) {
-    f32x4 score[2][R];
-    static_for<2>([&](auto B) {
-      static_for<R>([&](auto J) { score[decltype(B)::value][decltype(J)::value] = f32x4{0.f, 0.f, 0.f, 0.f}; });
-      static_for<KW>([&](auto Q) {
-        constexpr int b = decltype(B)::value, w = decltype(Q)::value;
-        if constexpr (w % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-        const u32x4 f = frags[buf][(2 * u + b) * KW + w][lane];
-        static_for<R>([&](auto J) { score[b][decltype(J)::value] = A::Op::run(f, a.q[decltype(J)::value][w], score[b][decltype(J)::value]); });
+  // A tile's sub-steps read their fragments in order, keys then values, AHEAD of them before they are multiplied.
+  constexpr int AHEAD = 4, SF = 2 * KW + NE, SLOTS = TT / 32 * SF, EVERY = SLOTS / PIECES;
+  auto compute = [&](int n, int buf, int bad) __attribute__((always_inline)) {
+    auto slot = [&](auto N) __attribute__((always_inline)) {
+      constexpr int k = decltype(N)::value;
+      if constexpr (k % EVERY == EVERY - 1 && k / EVERY < PIECES) piece(std::integral_constant<int, k / EVERY>{}, n + 1, buf ^ 1);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    static_for<TT / 32>([&](auto U) __attribute__((always_inline)) {
+      constexpr int u = decltype(U)::value;
+      const int t0 = n * TT + 32 * u, hid = bad >> (2 * u) & 3;
+      const bool mask = !(t0 >= see.all_lo && t0 + 31 <= see.all_hi && hid == 0);
+      u32x4 f[AHEAD];
+      auto read = [&](auto F) __attribute__((always_inline)) {
+        constexpr int k = decltype(F)::value;
+        if constexpr (k < SF) f[k % AHEAD] = frags[buf][k < 2 * KW ? 2 * u * KW + k : KF + u * NE + k - 2 * KW][lane];
+      };
+      static_for<AHEAD>([&](auto F) { read(F); });
+      f32x4 score[2][R];
+      static_for<2>([&](auto B) {
+        static_for<R>([&](auto J) { score[decltype(B)::value][decltype(J)::value] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+        static_for<KW>([&](auto Q) __attribute__((always_inline)) {
+          constexpr int b = decltype(B)::value, w = decltype(Q)::value, k = b * KW + w;
+          static_for<R>([&](auto J) { score[b][decltype(J)::value] = A::Op::run(f[k % AHEAD], a.q[decltype(J)::value][w], score[b][decltype(J)::value]); });
+          read(std::integral_constant<int, k + AHEAD>{});
+          slot(std::integral_constant<int, u * SF + k>{});
+        });
       });
-    });
-    u32x4 p[R];
-    a.weigh(score, p, t0, mask, bad, scale, lane);
-    static_for<NE>([&](auto E) {
-      constexpr int e = decltype(E)::value;
-      if constexpr (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-      const u32x4 f = frags[buf][KF + u * NE + e][lane];
-      static_for<R>([&](auto J) { a.acc[e][decltype(J)::value] = A::Op::run(f, p[decltype(J)::value], a.acc[e][decltype(J)::value]); });
+      u32x4 p[R];
+      a.weigh(score, p, t0, mask, hid, T.window, scale, lane);
+      static_for<NE>([&](auto E) __attribute__((always_inline)) {
+        constexpr int e = decltype(E)::value, k = 2 * KW + e;
+        static_for<R>([&](auto J) { a.acc[e][decltype(J)::value] = A::Op::run(f[k % AHEAD], p[decltype(J)::value], a.acc[e][decltype(J)::value]); });
+        read(std::integral_constant<int, k + AHEAD>{});
+        slot(std::integral_constant<int, u * SF + k>{});
+      });
     });
   };
   int bad_pages = 0;
   if (n0 < n1) {
-    auto held = [&](int n) { return n < n1 - 1 ? n : n1 - 1; };      // what is fetched ahead stays inside
-    Raw raw;
-    fetch(raw, n0, look_up(n0));
-    widen_tile(raw, n0, 0);
-    fetch(raw, held(n0 + 1), look_up(held(n0 + 1)));
-    Pages next = look_up(held(n0 + 2));
+    fetch(n0, look_up(n0));
+    next_page = look_up(n0 + 1 < n1 ? n0 + 1 : n1 - 1);
+    static_for<PIECES>([&](auto P) { piece(P, n0, 0); });
     __syncthreads();
     for (int n = n0; n < n1; ++n) {
       const int buf = (n - n0) & 1;
-      if (n + 1 < n1) widen_tile(raw, n + 1, buf ^ 1);
-      fetch(raw, held(n + 2), next);
-      next = look_up(held(n + 3));
-      if (n * TT <= see.hi && n * TT + TT - 1 >= see.lo) {
-#pragma unroll 1
-        for (int u = 0; u < TT / 32; ++u) {
-          const int t0 = n * TT + 32 * u, bad = __builtin_amdgcn_readfirstlane(hidden[buf][2 * u] | hidden[buf][2 * u + 1] << 1);
-          if (t0 + 16 <= all.hi) bad_pages |= bad;
-          else if (t0 <= all.hi) bad_pages |= bad & 1;
-          if (t0 <= see.hi && t0 + 31 >= see.lo) sub_step(!(t0 >= see.all_lo && t0 + 31 <= see.all_hi && bad == 0), buf, u, t0, bad);
-        }
-      }
+      next_page = look_up(n + 2 < n1 ? n + 2 : n1 - 1);
+      int bad = 0;
+      static_for<BLOCKS>([&](auto B) { bad |= hidden[buf][decltype(B)::value] << decltype(B)::value; });
+      bad = __builtin_amdgcn_readfirstlane(bad);
+      bad_pages |= bad & ((2 << ((all.hi - n * TT) / 16 < BLOCKS ? (all.hi - n * TT) / 16 : BLOCKS - 1)) - 1);      // of blocks up to the last token
+      compute(n, buf, bad);      // also where the wavefront's rows see none of it, a few tiles at a sequence's ends: one path keeps the sums in place
       __syncthreads();
     }
   }
@@ -481,7 +502,7 @@ __global__ __launch_bounds__(kAttnRowWaves * 64, D == 256 ? 1 : 2) void st_attn_
 // The wavefronts' results meet in LDS; where a sequence has several stretches their results meet in memory, and the last workgroup to
 // arrive joins them in order.
 template <int DT, int D, int R>
-__global__ __launch_bounds__(kAttnTokenWaves * 64) void st_attn_tokens_kernel(const AttnDev* table, const AttnItem* items) {
+__global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) void st_attn_tokens_kernel(const AttnDev* table, const AttnItem* items) {
   constexpr int W = kAttnTokenWaves, THREADS = W * 64, ROWS = 16 * R;
   constexpr int DP = D < 128 ? D : 128, PASS = D / DP, EP = DP / 16, kPitch = DP + 4;       // dims per pass
   __shared__ __align__(16) float part[W][16][kPitch];

@@ -60,7 +60,7 @@ constexpr int kAttnTokenWaves = 8, kAttnRowWaves = 4;
 constexpr int kAttnMaxSplit = 64;
 constexpr int kAttnTokens1 = 0, kAttnTokens2 = 1, kAttnRows = 2, kNumAttnKinds = 3;
 // R of a kind: rows are as many as the registers hold beside their queries, scores and outputs
-constexpr int attn_blocks(int kind, int dim) { return kind == kAttnTokens1 ? 1 : kind == kAttnTokens2 ? (dim == 256 ? 1 : 2) : dim == 64 ? 4 : dim == 128 ? 3 : 2; }
+constexpr int attn_blocks(int kind, int dim) { return kind == kAttnTokens1 ? 1 : kind == kAttnTokens2 ? (dim == 256 ? 1 : 2) : dim == 64 ? 4 : dim == 128 ? 3 : 1; }
 
 // Bytes of a block of 16 tokens of one head, and where its parts begin.
 constexpr int attn_block_bytes(int dim) { return kAttnBlock * (dim + dim / 16); }
