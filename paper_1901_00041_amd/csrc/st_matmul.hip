@@ -158,19 +158,26 @@ __device__ __forceinline__ u32x4 row_end(const void* p, int64_t row, int64_t row
 }
 
 // Publishes this workgroup's partial sums and returns whether it is the last of its tile, which then has the slices' sum, in slice
-// order.  get(q) / set(q, v): the thread's q-th group of four sums.  As in st_tiles.hpp: device-scope stores and loads, no L2-wide
+// order.  get(q) / set(q, v): the thread's q-th group of four sums, at 16 (q THREADS + thread) bytes of its slice; a slice is as long as the
+// tile's fp32 sums, SLICE bytes, and a group past its end is not one of the tile's.  As in st_tiles.hpp: device-scope stores and loads, no L2-wide
 // fence, nobody waits.
-template <int NQ, int THREADS, class Get, class Set>
+template <int NQ, int THREADS, uint32_t SLICE, class Get, class Set>
 __device__ __forceinline__ bool join_slices(ConstMatmul& T, const MatmulItem it, Get&& get, Set&& set, uint32_t* flag) {
   const int tid = (int)threadIdx.x, split = T.split;
   const int64_t tile = (int64_t)it.tile_m * T.tiles_n + it.tile_n;
-  constexpr uint32_t kSlice = NQ * THREADS * 16;
-  float* base = T.ws + tile * split * (kSlice / 4);
-  const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, (uint32_t)split * kSlice);
+  static_assert(SLICE == NQ * THREADS * 16u || (NQ == 1 && SLICE < THREADS * 16u), "groups fill a slice, or one is enough");
+  float* base = T.ws + tile * split * (SLICE / 4);
+  const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, (uint32_t)split * SLICE);
+  // A group's place is the thread's plus a scalar.  Nothing but scalar instructions may come between these stores and the wait: a vector
+  // instruction right behind a store with a scalar offset has been seen to overwrite registers that the store had still to read
+  // (two values of eight lanes, in one run out of three of a 256x256 fp32 tile), and the compiler puts no distance between such two.
+  const uint32_t mine = (uint32_t)(tid * 16) < SLICE ? (uint32_t)(tid * 16) : kInvalidOffset;
+  __builtin_amdgcn_sched_barrier(0);
   static_for<NQ>([&](auto Q) {
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, get(Q)), rs, (decltype(Q)::value * THREADS + tid) * 16, (int)(it.slice * kSlice), kAuxDeviceCoherent);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, get(Q)), rs, (int)mine, (int)(it.slice * SLICE) + decltype(Q)::value * THREADS * 16, kAuxDeviceCoherent);
   });
   __builtin_amdgcn_s_waitcnt(0);
+  __builtin_amdgcn_sched_barrier(0);
   __syncthreads();
   if (tid == 0) {
     const uint32_t old = __hip_atomic_fetch_add(&T.counters[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -193,8 +200,8 @@ __device__ __forceinline__ bool join_slices(ConstMatmul& T, const MatmulItem it,
       for (int s = 0; s < SB; ++s)
 #pragma unroll
         for (int q = 0; q < QB; ++q) {
-          const uint32_t off = s0 + s < split ? (uint32_t)(((q0 + q) * THREADS + tid) * 16) : kInvalidOffset;
-          part[s][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, (s0 + s) * (int)kSlice, kAuxDeviceCoherent));
+          const uint32_t off = s0 + s < split ? mine : kInvalidOffset;
+          part[s][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, (s0 + s) * (int)SLICE + (q0 + q) * THREADS * 16, kAuxDeviceCoherent));
         }
 #pragma unroll
       for (int s = 0; s < SB; ++s)
@@ -297,7 +304,7 @@ __global__ __launch_bounds__(256) void st_matmul_skinny_kernel(const MatmulDev* 
     v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (q < R * F) v[k] = (part[0][q][lane] + part[1][q][lane]) + (part[2][q][lane] + part[3][q][lane]);
   }
-  if (T.split > 1 && !join_slices<NQ, 256>(T, it, [&](auto Q) { return v[decltype(Q)::value]; }, [&](auto Q, f32x4 s) { v[decltype(Q)::value] = s; }, &flag)) return;
+  if (T.split > 1 && !join_slices<NQ, 256, R * F * 1024>(T, it, [&](auto Q) { return v[decltype(Q)::value]; }, [&](auto Q, f32x4 s) { v[decltype(Q)::value] = s; }, &flag)) return;
 #pragma unroll
   for (int k = 0; k < NQ; ++k) {
     const int q = k * 4 + wave;
@@ -431,7 +438,7 @@ __global__ __launch_bounds__(WM * WN * 64) void st_matmul_tile_kernel(const Matm
       constexpr int q = decltype(Q)::value, j = q / 4 / BM, i = q / 4 % BM, g = q % 4;
       acc[j][i][4 * g] = v[0], acc[j][i][4 * g + 1] = v[1], acc[j][i][4 * g + 2] = v[2], acc[j][i][4 * g + 3] = v[3];
     };
-    if (!join_slices<BN * BM * 4, THREADS>(T, it, get, set, &flag)) return;
+    if (!join_slices<BN * BM * 4, THREADS, MT * NT * 4>(T, it, get, set, &flag)) return;
   }
   // A wavefront turns its rows round in LDS of its own, 32 of them at a time, so that a row's outputs leave together.
   float* mine = (float*)smem + wave * 32 * kPitch;

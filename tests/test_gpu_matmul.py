@@ -150,6 +150,23 @@ def test_every_tile_shape(cfg, dtype, split):
         p.check(f"{m}x{n}x{k} again")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cfg", range(7))
+def test_slices_of_many_tiles_stay_apart(cfg, dtype):
+    """Divided reductions of many tiles at once: a slice's partial sums take their tile's room in the workspace and no more."""
+    mt, nt = st_lm.st_matmul_tile_shape(cfg)
+    tenants = [Product(min(mt, 64), 40 * nt - 3, 1024, dtype, dtype, seed=s) for s in range(3)]
+    plan = run(tenants, tile_cfg=cfg + 1, split_k=8)
+    tiles = sum(st_lm.st_matmul_get_tenant_info(plan, t).tiles_m * st_lm.st_matmul_get_tenant_info(plan, t).tiles_n for t in range(3))
+    assert st_lm.st_matmul_get_info(plan).workspace_bytes == tiles * (8 * mt * nt * 4 + 4)
+    for turn in range(3):
+        for i, p in enumerate(tenants):
+            p.check(f"turn {turn}, tenant {i}")
+            p.whole_y.fill_(float("nan"))
+        st_lm.st_matmul_run(plan)
+        torch_().cuda.synchronize()
+
+
 @pytest.mark.parametrize("act, bias, residual", [c for c in itertools.product(ACTS, (False, True), ("none", "before", "last")) if c[1] or c[2] != "none" or c[0] != "none"])
 def test_epilogues(act, bias, residual):
     tenants = [Product(m, 72, 96, d, o, act=act, bias=bias, residual=residual, gain=4.0) for m in (2, 40, 70) for d, o in (("bf16", "bf16"), ("f16", "f32"), ("f32", "f32"))]
