@@ -80,48 +80,105 @@ void set_pointers(MatmulDev& T, const st_matmul_desc& d, const st_matmul_desc& p
 }
 
 // ---- choice of a tile shape and of a division of the reduction -----------------------------------------------------------
-struct Choice { int shape, split, per_split; double clocks; };
+// Microseconds of a launch of one shape: a workgroup alone takes first + steps step, a compute unit through which many pass busy_first +
+// steps busy_step for each; a divided reduction adds join and join_kb for each KiB of the tile's partial sums (and busy_kb per KiB of a
+// slice); the operands come at 5 TB/s.  The largest of the three is the time, the others weigh a little.  Constants fitted to 193
+// products of 1 to 4096 rows, 64 to 8192 outputs and inputs and 1 to 16 tenants, each measured with every shape and up to seven
+// divisions: what it picks takes 1.5 % longer in the geometric mean than the fastest of them.  [shape][fp32]
+struct Cost { double first, step, busy_first, busy_step, join, join_kb, busy_kb; };
+constexpr Cost kCosts[kNumMatmulShapes][2] = {
+    {{3.36, 1.23, 16.2, 1.52, 6.98, 0.0619, 0.0383}, {8.18, 15.7, 0.0289, 9.24, 1.9e-05, 0.00505, 0.128}},
+    {{4.85, 0.511, 3.59, 0.521, 8.86, 0.0166, 0.0742}, {38.6, 0.806, 0.393, 1.4, 4.33, 0.0135, 0.268}},
+    {{0.925, 0.195, 0.975, 0.296, 1.13, 0.0111, 0.131}, {1.09, 0.415, 2.01, 0.487, 1.2, 0.0104, 0.0732}},
+    {{3.84, 0.145, 1.48, 1.23, 0.707, 0.0756, 0.119}, {6.19, 0.468, 1.23, 1.36, 1.06, 0.00445, 4.56e-09}},
+    {{1.23, 0.315, 0.527, 0.501, 0.347, 0.0287, 0.901}, {2.85, 0.109, 0.949, 1.23, 1.22, 0.0207, 5.71e-09}},
+    {{0.896, 0.22, 0.731, 0.394, 0.964, 0.0708, 0.471}, {1.55, 0.153, 0.768, 0.541, 1.23, 0.106, 4.4e-08}},
+    {{1.02, 0.0846, 1.3, 0.179, 0.551, 0.198, 0.703}, {1.73, 0.0781, 2.17, 0.0348, 0.793, 0.213, 0.0953}},
+};
+constexpr double kLaunchUs = 2.0;      // ... and what a launch takes beside them
+constexpr int kMostSplit = 32;
 
 int steps_of(const st_matmul_desc& d, int shape) {
   const int bytes = kMatmulShapes[shape].skinny ? kMatmulUnitBytes : kMatmulStepBytes;
   return cdiv((int64_t)(d.K / (16 / elem_size(d.in_dtype))) * 16, bytes);
 }
-
-// Clocks until a tenant is done that has `share` of the chip to itself.
-double clocks_of(const st_matmul_desc& d, int shape, int split, double share) {
+// A tenant's least time, in the share of the chip that it needs of its launch: what it takes at the rates of the matrix cores and of memory.
+double work_of(const st_matmul_desc& d) {
+  const double es = elem_size(d.in_dtype), flops = 2.0 * d.M * d.N * d.K;
+  return std::max(flops / (es == 4 ? 1.3e8 : 1.3e9), ((double)d.M * d.K + (double)d.N * d.K + (double)d.M * d.N) * es / 5e6);
+}
+double time_of(const st_matmul_desc& d, int shape, int split, double share) {
   const MatmulShape& S = kMatmulShapes[shape];
-  const int steps = steps_of(d, shape), per = std::max(1, cdiv(steps, split)), es = elem_size(d.in_dtype);
-  const int64_t items = (int64_t)cdiv(d.M, S.MT) * cdiv(d.N, S.NT) * split;
-  double item, resident;
-  if (S.skinny) {
-    const int in_flight = 2 * (S.MT / 16 + S.NT / 16 <= 2 ? 8 : S.MT / 16 + S.NT / 16 <= 4 ? 4 : 2);
-    resident = 2;
-    const double unit = std::max(2000.0 / in_flight, (S.MT + S.NT) * 64 * 4.0 * resident / 40.0 / 4.0);
-    item = 2500 + cdiv(per, 4) * unit;
-  } else {
-    const double mfma = (double)S.MT * S.NT * (kMatmulStepBytes / es) * 2 / (es == 4 ? 256 : 4096) / 0.75, load = (S.MT + S.NT) * 128 / 40.0;
-    resident = shape == 0 ? 1 : 2;
-    item = 3500 + S.MT * S.NT / 12.0 + per * std::max(resident * std::max(mfma, load), shape == 2 ? 450.0 : 900.0);
-  }
-  if (split > 1) item += 2000 + split * S.MT * S.NT * 4 / 64.0;
-  const double rounds = std::max(1.0, std::ceil(items / (kNumCUs * resident * share) - 1e-9));
-  return std::max(rounds * item, ((double)d.N * d.K + (double)d.M * d.K) * es / (2200 * share));
+  const bool f32 = d.in_dtype == ST_DT_F32;
+  const Cost& c = kCosts[shape][f32];
+  const int steps = std::max(1, cdiv(std::max(1, steps_of(d, shape)), split * (S.skinny ? 4 : 1)));
+  const double items = (double)cdiv(d.M, S.MT) * cdiv(d.N, S.NT) * split / (kNumCUs * share), kb = S.MT * S.NT * 4 / 1024.0;
+  const double alone = c.first + steps * c.step + (split > 1 ? c.join + c.join_kb * split * kb : 0.0);
+  const double busy = items * (c.busy_first + steps * c.busy_step + (split > 1 ? c.busy_kb * kb : 0.0));
+  const double memory = ((double)d.N * d.K + (double)d.M * d.K) * elem_size(d.in_dtype) / (5e6 * share), most = std::max(alone, busy);
+  return std::max(most, memory) + 0.25 * std::min(alone, busy) + 0.3 * std::min(memory, most);
 }
 
-Choice choose(const st_matmul_desc& d, double share, const st_plan_opts& o) {
-  Choice best = {-1, 1, 1, 0};
-  for (int shape = 0; shape < kNumMatmulShapes; ++shape) {
-    const MatmulShape& S = kMatmulShapes[shape];
-    if (o.tile_cfg ? o.tile_cfg - 1 != shape : (S.skinny && (d.M > S.MT || (d.M <= S.MT / 2 && S.MT > 16)))) continue;
-    const int steps = steps_of(d, shape);
-    for (int want = 1; want <= 32; ++want) {
-      if (o.split_k && want != 1) break;
-      int split = std::max(1, std::min(o.split_k ? o.split_k : want, steps));
-      const int per = std::max(1, cdiv(steps, split));
-      split = std::max(1, cdiv(steps, per));
-      const Choice c = {shape, split, per, clocks_of(d, shape, split, share)};
-      if (best.shape < 0 || c.clocks < best.clocks) best = c;
+struct Choice { int shape, split, per_split; };
+
+// The division of the reduction that suits a tenant best in a shape, and its time.
+Choice divide(const st_matmul_desc& d, int shape, double share, int forced, double* time) {
+  const int steps = std::max(1, steps_of(d, shape));
+  Choice best = {shape, 1, steps};
+  *time = -1;
+  for (int want = forced ? forced : 1; want <= (forced ? forced : kMostSplit); ++want) {
+    const int per = cdiv(steps, std::min(want, steps)), split = cdiv(steps, per);
+    const double t = time_of(d, shape, split, share);
+    if (*time < 0 || t < *time) best = {shape, split, per}, *time = t;
+  }
+  return best;
+}
+
+// Shapes and divisions for tenants of one operand type.  Tenants of one shape go in one launch and share the chip by their work; launches run
+// one after the other.  Either all take the same shape, whichever is best for them together, or each the one that is best for it alone.
+double plan_together(const std::vector<st_matmul_desc>& descs, const std::vector<int>& who, const std::vector<int>& shape, int forced, std::vector<Choice>* out) {
+  double total = 0;
+  for (int s = 0; s < kNumMatmulShapes; ++s) {
+    double work = 0, longest = -1;
+    for (size_t i = 0; i < who.size(); ++i)
+      if (shape[i] == s) work += work_of(descs[who[i]]);
+    for (size_t i = 0; i < who.size(); ++i) {
+      if (shape[i] != s) continue;
+      double t;
+      (*out)[i] = divide(descs[who[i]], s, std::max(work_of(descs[who[i]]) / work, 1e-4), forced, &t);
+      longest = std::max(longest, t);
     }
+    if (longest >= 0) total += kLaunchUs + longest;
+  }
+  return total;
+}
+// Skinny tiles are for tenants whose rows one of them holds.
+bool holds_rows(const st_matmul_desc& d, int shape) { return !kMatmulShapes[shape].skinny || d.M <= kMatmulShapes[shape].MT; }
+std::vector<Choice> choose(const std::vector<st_matmul_desc>& descs, const std::vector<int>& who, const st_plan_opts& o) {
+  std::vector<Choice> best(who.size()), now(who.size());
+  std::vector<int> shape(who.size());
+  double least = -1;
+  auto look = [&] {
+    const double t = plan_together(descs, who, shape, o.split_k, &now);
+    if (least < 0 || t < least) best = now, least = t;
+  };
+  for (int s = 0; s < kNumMatmulShapes; ++s) {
+    if (o.tile_cfg && s != o.tile_cfg - 1) continue;
+    std::fill(shape.begin(), shape.end(), s);
+    if (o.tile_cfg || std::all_of(who.begin(), who.end(), [&](int t) { return holds_rows(descs[t], s); })) look();
+  }
+  if (!o.tile_cfg && who.size() > 1) {
+    double work = 0;
+    for (int t : who) work += work_of(descs[t]);
+    for (size_t i = 0; i < who.size(); ++i) {
+      double mine = -1, t;
+      for (int s = 0; s < kNumMatmulShapes; ++s) {
+        if (!holds_rows(descs[who[i]], s)) continue;
+        divide(descs[who[i]], s, std::max(work_of(descs[who[i]]) / work, 1e-4), o.split_k, &t);
+        if (mine < 0 || t < mine) shape[i] = s, mine = t;
+      }
+    }
+    look();
   }
   return best;
 }
@@ -181,21 +238,18 @@ st_status build(st_matmul* p, const st_matmul_desc* descs, int n, const st_plan_
   p->tenants.assign((size_t)n, MatmulDev{});
   p->totals.n_tenants = n;
   p->totals.host_only = o.host_only;
-  std::vector<double> work((size_t)n, 0.0), clocks((size_t)n, 0.0);
-  double all = 0;
-  for (int t = 0; t < n; ++t) {
-    const st_matmul_desc& d = descs[t];
-    const int64_t es = elem_size(d.in_dtype), os = elem_size(d.out_dtype);
-    if (d.M == 0) continue;
-    const double flops = 2.0 * d.M * d.N * d.K;
-    const int64_t bytes = ((int64_t)d.M * d.K + (int64_t)d.N * d.K + ((d.epilogue & ST_EPI_BIAS) ? d.N : 0)) * es + (int64_t)d.M * d.N * os * ((d.epilogue & kResiduals) ? 2 : 1);
-    p->totals.flops += 2 * (int64_t)d.M * d.N * d.K;
-    p->totals.bytes += bytes;
-    work[t] = std::max(flops / (es == 4 ? 256 : 4096) / kNumCUs, bytes / 2200.0);
-    all += work[t];
+  std::vector<Choice> choice((size_t)n, Choice{0, 1, 1});
+  for (int dtype = 0; dtype < 3; ++dtype) {
+    std::vector<int> who;
+    for (int t = 0; t < n; ++t)
+      if (descs[t].in_dtype == dtype && descs[t].M > 0) who.push_back(t);
+    if (who.empty()) continue;
+    const std::vector<Choice> c = choose(p->descs, who, o);
+    for (size_t i = 0; i < who.size(); ++i) choice[(size_t)who[i]] = c[i];
   }
   for (int t = 0; t < n; ++t) {
     const st_matmul_desc& d = descs[t];
+    const int64_t es = elem_size(d.in_dtype), os = elem_size(d.out_dtype);
     st_matmul_tenant_info& ti = p->info[t];
     MatmulDev& T = p->tenants[t];
     T.M = d.M; T.N = d.N; T.K = d.K;
@@ -203,17 +257,19 @@ st_status build(st_matmul* p, const st_matmul_desc* descs, int n, const st_plan_
     T.epilogue = d.epilogue;
     T.out_f32 = d.out_dtype == ST_DT_F32;
     set_pointers(T, d, d);
-    const Choice c = choose(d, all > 0 ? std::max(work[t] / all, 1.0 / 4096) : 1.0, o);
+    const Choice& c = choice[(size_t)t];
     const MatmulShape& S = kMatmulShapes[c.shape];
     ti.tile_cfg = c.shape;
     ti.MT = S.MT; ti.NT = S.NT;
     ti.tiles_m = cdiv(d.M, S.MT); ti.tiles_n = cdiv(d.N, S.NT);
-    ti.split_k = d.M ? c.split : 1;
+    ti.split_k = c.split;
     if ((double)ti.tiles_m * ti.tiles_n * ti.split_k >= 2147483648.0) return fail(ST_ERR_UNSUPPORTED, "tenant %d: more than 2^31 work items", t);
     ti.item_count = (int64_t)ti.tiles_m * ti.tiles_n * ti.split_k;
     T.tiles_n = ti.tiles_n; T.split = ti.split_k; T.per_split = c.per_split;
-    clocks[t] = c.clocks;
     p->totals.n_items += ti.item_count;
+    if (d.M == 0) continue;
+    p->totals.flops += 2 * (int64_t)d.M * d.N * d.K;
+    p->totals.bytes += ((int64_t)d.M * d.K + (int64_t)d.N * d.K + ((d.epilogue & ST_EPI_BIAS) ? d.N : 0)) * es + (int64_t)d.M * d.N * os * ((d.epilogue & kResiduals) ? 2 : 1);
   }
   if (p->totals.n_items >= ((int64_t)1 << 31)) return fail(ST_ERR_UNSUPPORTED, "more than 2^31 work items");
   for (int dtype = 0; dtype < 3; ++dtype)

@@ -71,7 +71,7 @@ class _Owned:
         self.handle, self._keep = handle, keep
 
     def destroy(self):
-        if getattr(self, "handle", None) and sc._lib is not None:
+        if getattr(self, "handle", None):
             try:
                 getattr(sc._lib, self._destroy)(self.handle)
             except Exception:      # interpreter shutdown
