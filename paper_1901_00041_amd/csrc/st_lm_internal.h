@@ -27,9 +27,6 @@ constexpr int kMatmulStepBytes = 128;    // of a row, per step of a tile through
 constexpr int kMatmulUnitBytes = 64;     // of a row, per MFMA step of a skinny tile
 constexpr int kMatmulMaxK = 1 << 20, kMatmulMaxLd = 1 << 21;     // a tile's rows stay below 2^31 bytes
 
-// How a tenant's outputs, residual and bias are reached: 16 bytes at a time where address and row length allow it.
-constexpr uint32_t kMatmulVecY = 1u, kMatmulVecRes = 2u, kMatmulVecBias = 4u;
-
 struct MatmulDev {
   const void* x;
   const void* w;
@@ -40,10 +37,10 @@ struct MatmulDev {
   uint32_t* counters;    // one arrival counter per output tile, zero between runs
   int32_t M, N, K;
   int32_t ldx, ldw, ldy, ldr;
-  uint32_t epilogue, vec;
+  uint32_t epilogue;
   int32_t out_f32;
   int32_t tiles_n, split, per_split;   // per_split: steps (units of a skinny tile) per slice
-  int32_t pad[5];
+  int32_t pad[6];
 };
 static_assert(sizeof(MatmulDev) == 128, "two lines of the scalar cache, a multiple of 16 bytes for launch_poke");
 

@@ -74,9 +74,6 @@ void set_pointers(MatmulDev& T, const st_matmul_desc& d, const st_matmul_desc& p
   T.x = p.x; T.w = p.w; T.y = p.y;
   T.bias = (d.epilogue & ST_EPI_BIAS) ? p.bias : nullptr;
   T.res = (d.epilogue & kResiduals) ? p.residual : nullptr;
-  const int64_t os = elem_size(d.out_dtype);
-  auto aligned = [](const void* q, int64_t ld_bytes) { return (uintptr_t)q % 16 == 0 && ld_bytes % 16 == 0; };
-  T.vec = (aligned(T.y, T.ldy * os) ? kMatmulVecY : 0u) | (aligned(T.res, T.ldr * os) ? kMatmulVecRes : 0u) | (aligned(T.bias, 0) ? kMatmulVecBias : 0u);
 }
 
 // ---- choice of a tile shape and of a division of the reduction -----------------------------------------------------------

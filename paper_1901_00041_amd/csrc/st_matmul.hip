@@ -65,25 +65,32 @@ __device__ __forceinline__ void activate(uint32_t epi, float (&v)[W]) {
   }
 }
 
-// W (4 or 8) consecutive values of one row, from 16-byte (or, four 16-bit ones, 8-byte) aligned memory
+// Vectors at any address that is a multiple of the element's size: the hardware takes them, and one such access costs less than one per element.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
+// W (4 or 8) consecutive values of one row
 template <int DT, int W>
 __device__ __forceinline__ void load_row(const void* p, int64_t i, bool f32, float (&v)[W]) {
   if (DT == ST_DT_F32 || f32) {
 #pragma unroll
     for (int q = 0; q < W / 4; ++q) {
-      const f32x4 a = *(const f32x4*)((const float*)p + i + 4 * q);
+      const f32x4 a = *(const f32x4_any*)((const float*)p + i + 4 * q);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[4 * q + e] = a[e];
     }
   } else {
-#pragma unroll
-    for (int q = 0; q < W / 4; ++q) {
-      const uint2 a = *(const uint2*)((const uint16_t*)p + i + 4 * q);
-      v[4 * q] = unpack16<DT>(a.x, 0);
-      v[4 * q + 1] = unpack16<DT>(a.x, 1);
-      v[4 * q + 2] = unpack16<DT>(a.y, 0);
-      v[4 * q + 3] = unpack16<DT>(a.y, 1);
+    uint32_t a[W / 2];
+    if constexpr (W == 8) {
+      const u32x4 b = *(const u32x4_any*)((const uint16_t*)p + i);
+      a[0] = b[0], a[1] = b[1], a[2] = b[2], a[3] = b[3];
+    } else {
+      const u32x2_any b = *(const u32x2_any*)((const uint16_t*)p + i);
+      a[0] = b[0], a[1] = b[1];
     }
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = unpack16<DT>(a[e / 2], e & 1);
   }
 }
 
@@ -95,22 +102,20 @@ struct RowEnd {
   int64_t ldr, ldy;
   uint32_t epi;
   int n, left;            // outputs that there are from n on
-  bool f32, vec_res, vec_y;
+  bool f32, whole;
   float bias[W];
 
   __device__ __forceinline__ RowEnd(ConstMatmul& T, int first) {
     n = first;
     left = T.N - n;
-    const uint32_t vec = T.vec;
-    const bool whole = left >= W;
+    whole = left >= W;
     epi = T.epilogue;
     f32 = DT == ST_DT_F32 || T.out_f32 != 0;
-    vec_res = whole && (vec & kMatmulVecRes), vec_y = whole && (vec & kMatmulVecY);
     res = T.res, y = T.y, ldr = T.ldr, ldy = T.ldy;
 #pragma unroll
     for (int e = 0; e < W; ++e) bias[e] = 0.f;
     if (left > 0 && (epi & ST_EPI_BIAS)) {
-      if (whole && (vec & kMatmulVecBias)) {
+      if (whole) {
         load_row<DT, W>(T.bias, n, false, bias);
       } else {
 #pragma unroll
@@ -125,7 +130,7 @@ struct RowEnd {
     float r[W];
     if (epi & (ST_EPI_RESIDUAL | ST_EPI_RESIDUAL_LAST)) {
       const int64_t at = m * ldr + n;
-      if (vec_res) {
+      if (whole) {
         load_row<DT, W>(res, at, f32, r);
       } else {
 #pragma unroll
@@ -144,9 +149,9 @@ struct RowEnd {
     const int64_t at = m * ldy + n;
     if (f32) {
       float* to = (float*)y + at;
-      if (vec_y) {
+      if (whole) {
 #pragma unroll
-        for (int q = 0; q < W / 4; ++q) *(f32x4*)(to + 4 * q) = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        for (int q = 0; q < W / 4; ++q) *(f32x4_any*)(to + 4 * q) = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
       } else {
 #pragma unroll
         for (int e = 0; e < W; ++e)
@@ -157,9 +162,9 @@ struct RowEnd {
       uint32_t o[W / 2];
 #pragma unroll
       for (int e = 0; e < W / 2; ++e) o[e] = pack16<DT>(v[2 * e], v[2 * e + 1]);
-      if (vec_y) {
-        if constexpr (W == 8) *(u32x4*)to = u32x4{o[0], o[1], o[2], o[3]};
-        else *(uint2*)to = make_uint2(o[0], o[1]);
+      if (whole) {
+        if constexpr (W == 8) *(u32x4_any*)to = u32x4{o[0], o[1], o[2], o[3]};
+        else *(u32x2_any*)to = u32x2_any{o[0], o[1]};
       } else {
 #pragma unroll
         for (int e = 0; e < W; ++e)
@@ -169,17 +174,27 @@ struct RowEnd {
   }
 };
 
-// The elements of a row behind its whole 16-byte chunks, as one chunk; zeros for a row that there is not.
+// The elements of a row behind its whole 16-byte chunks, as one chunk; zeros for a row that there is not.  Where the row is as long as a
+// chunk, it is the row's last one with what the whole chunks have cleared: the same places in both operands.
 template <int DT>
 __device__ __forceinline__ u32x4 row_end(const void* p, int64_t row, int64_t rows, int ld, int K, bool mine) {
   constexpr int ES = ElemOf<DT>::ES, VEC = 16 / ES;
-  const int whole = K / VEC * VEC;
   u32x4 out = {0u, 0u, 0u, 0u};
   if (!mine || row >= rows) return out;
+  const int left = K % VEC;
+  if (K >= VEC) {
+    const u32x4 v = *(const u32x4_any*)((const char*)p + (row * ld + K - VEC) * ES);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const uint32_t keep = ES == 4 ? (d >= VEC - left ? 0xffffffffu : 0u) : (2 * d >= VEC - left ? 0x0000ffffu : 0u) | (2 * d + 1 >= VEC - left ? 0xffff0000u : 0u);
+      out[d] = v[d] & keep;
+    }
+    return out;
+  }
 #pragma unroll
   for (int e = 0; e < VEC - 1; ++e) {
-    if (whole + e < K) {
-      const int64_t i = row * ld + whole + e;
+    if (e < K) {
+      const int64_t i = row * ld + e;
       if constexpr (ES == 4) out[e] = ((const uint32_t*)p)[i];
       else out[e >> 1] |= (uint32_t)((const uint16_t*)p)[i] << (16 * (e & 1));
     }
