@@ -160,7 +160,7 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
     // 0, or so small, counts as 2^-100, under which all finite scores are equal, too
     T.scale = std::max(std::fabs(d.scale) * 1.44269504088896340736f, 7.888609e-31f);
     T.flip = d.scale < 0 ? 0x80008000u : 0u;
-    T.row_tiles = cdiv(most_rows(d), (kind == kAttnRows ? kAttnRowWaves : 1) * 16 * attn_blocks(kind, d.head_dim));
+    T.row_tiles = cdiv(most_rows(d), (kind == kAttnRows ? attn_row_waves(d.head_dim) : 1) * 16 * attn_blocks(kind, d.head_dim));
     T.split = 1;
     T.chunk = 1 << 30;
     if (d.max_tokens > 0 && kind != kAttnRows) tiles += (double)d.n_seqs * d.kv_heads * T.row_tiles;

@@ -6,7 +6,7 @@
 //            hold the same ones.  The result leaves a lane with the scores of query row i for tokens 4g .. 4g+3.
 //   values   O^T = V^T P^T, dims x query rows, over 32 tokens: the weights of two blocks as they stand are operand B (tokens 4g .. 4g+3 of
 //            both), and the values' codes are stored so that a lane reads, as one vector, the same four tokens of dim / 16 elements.
-//   sums     of the weights, as they were rounded: an MFMA with ones.
+//   sums     of the weights, as they were rounded, lane by lane.
 // Elements E2M1 become 16-bit ones, scaled, in v_cvt_scalef32_pk_*_fp4 (exact).  The softmax runs in one pass; its reference is raised, and
 // what has been summed scaled down, only when a score exceeds it by 2^kLag, so that most steps need nothing from another lane.
 #include <hip/hip_runtime.h>
@@ -99,13 +99,27 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
 // The larger of two values in one instruction: as a median with an infinity that the compiler does not know (fmaxf of what an MFMA left
 // costs another one per operand, which quiets NaNs).
 __device__ __forceinline__ float max_raw(float a, float b, float inf) { return __builtin_amdgcn_fmed3f(a, b, inf); }
+// sum + both of a pair
+template <int DT>
+__device__ __forceinline__ float add_pair(uint32_t pair, float sum) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  if constexpr (DT == ST_DT_BF16) return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
+  else return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), __builtin_bit_cast(f16x2, 0x3c003c00u), sum, false);
+}
+__device__ __forceinline__ float sum_of_row(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
 __device__ __forceinline__ float max_of_row(float v) {      // over the four lanes that hold a query row
   v = fmaxf(v, __shfl_xor(v, 16));
   return fmaxf(v, __shfl_xor(v, 32));
 }
 
 // ---- one wavefront's rows over a stretch of tokens -----------------------------------------------------------------------
-template <int DT, int D, int R>
+// MFMA_SUMS: the weights' sums by an MFMA with ones, which costs the fewest instructions where the vector unit is short (six prompts 454 us ->
+// 444); else by dot products, which costs the fewest registers (64 single tokens 70.6 us -> 67.2).
+template <int DT, int D, int R, bool MFMA_SUMS>
 struct Attend {
   static constexpr int KW = D / 32;        // dwords of a key quarter; MFMAs per score block
   static constexpr int VW = D / 32;        // dwords of four tokens' group of values
@@ -114,12 +128,13 @@ struct Attend {
   // Weights are 2^(score - m) with m lagging behind the true maximum by at most kLag; in fp16 they are moved up to the end of the type's
   // range, so that a weight has all its bits down to 2^-25 of the largest.
   static constexpr float kLag = DT == ST_DT_BF16 ? 8.f : 5.f, kUp = DT == ST_DT_BF16 ? 0.f : 10.f;
-  static constexpr float kNothing = -3.0e38f;
   static constexpr uint32_t kOnes = DT == ST_DT_BF16 ? 0x3f803f80u : 0x3c003c00u;
+  static constexpr float kNothing = -3.0e38f;
   typedef Mma<DT, 16> Op;
 
   u32x4 q[R][KW];
-  f32x4 acc[NE][R], sum[R];
+  f32x4 acc[NE][R];
+  f32x4 sum[R];            // MFMA_SUMS: each of them the row's; else [0] is that of the lane's own weights
   float m[R];              // reference, less kUp; kNothing: the row has seen no token yet
   int pos[R];              // the lane's rows' tokens; a row that there is not has queries of 0 and is not stored
 
@@ -129,6 +144,7 @@ struct Attend {
   };
   struct Pages { int p[2]; };
 
+  __device__ __forceinline__ float row_sum(int r) const { return MFMA_SUMS ? sum[r][0] : sum_of_row(sum[r][0]); }
   __device__ __forceinline__ void clear() {
     static_for<R>([&](auto J) {
       constexpr int r = decltype(J)::value;
@@ -226,7 +242,8 @@ struct Attend {
         auto weight = [&](int e) { return __builtin_amdgcn_exp2f(__builtin_fmaf(score[x / 2][r][e], scale, -m[r])); };
         p[r][x] = pack_pair<DT>(weight(x % 2 * 2), weight(x % 2 * 2 + 1));
       });
-      sum[r] = Op::run(u32x4{kOnes, kOnes, kOnes, kOnes}, p[r], sum[r]);
+      if constexpr (MFMA_SUMS) sum[r] = Op::run(u32x4{kOnes, kOnes, kOnes, kOnes}, p[r], sum[r]);
+      else static_for<4>([&](auto X) { sum[r][0] = add_pair<DT>(p[r][decltype(X)::value], sum[r][0]); });
     });
   }
 
@@ -335,13 +352,13 @@ __device__ __forceinline__ void store_out(ConstAttn& T, const Seq& S, int head, 
 // barrier a tile.  A wavefront issues a vector instruction every five to six clocks at best and its MFMAs take sixteen each, so the
 // widening is cut into pieces that are issued between MFMAs.
 template <int DT, int D, int R>
-__global__ __launch_bounds__(kAttnRowWaves * 64, 2) void st_attn_rows_kernel(const AttnDev* table, const AttnItem* items) {
-  typedef Attend<DT, D, R> A;
-  constexpr int W = kAttnRowWaves, TT = D == 256 ? 32 : 64, BLOCKS = TT / 16, KW = A::KW, NE = A::NE;
+__global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel(const AttnDev* table, const AttnItem* items) {
+  typedef Attend<DT, D, R, true> A;
+  constexpr int W = attn_row_waves(D), TT = D == 256 ? 32 : 64, BLOCKS = TT / 16, KW = A::KW, NE = A::NE;
   constexpr int SHARE = W / BLOCKS;                                     // wavefronts to a block
   constexpr int KWAVE = KW / SHARE, VWAVE = NE / SHARE;                 // fragments that a wavefront makes of its block's keys and values
   constexpr int KF = BLOCKS * KW, VF = TT / 32 * NE;                    // fragments of a tile
-  static_assert(W % BLOCKS == 0 && KW % SHARE == 0 && (KWAVE == 2 || KWAVE == 4), "whole fragments");
+  static_assert(W % BLOCKS == 0 && (D == 256 ? SHARE == 4 : SHARE == 1) && (KWAVE == 2 || KWAVE == 4), "a part is whole fragments, and lies in one word of a token's codes");
   __shared__ __align__(16) u32x4 frags[2][KF + VF][64];
   __shared__ __align__(16) int hidden[2][BLOCKS];
   const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
@@ -365,8 +382,8 @@ __global__ __launch_bounds__(kAttnRowWaves * 64, 2) void st_attn_rows_kernel(con
   struct Raw { uint32_t k[KWAVE], v[4], ks, vs; int page; };            // the part as it lies in the cache; v: a word per token (D = 64: per two)
   Raw raw;
   Table pages_of(T, seq, n0 < n1 ? n0 * TT : 0, n0 < n1 ? all.hi : 0, lane);
-  const uint32_t k_at = (uint32_t)(i * (D / 2) + g * (D / 8) + part * KWAVE * 4), v_at = (uint32_t)(8 * D + (i * 16 + 4 * g) * (D / 32) + part * 4);
-  const uint32_t ks_at = (uint32_t)(16 * D + i * (D / 32) + (D == 64 ? g / 2 : D == 128 ? g : 2 * g + part));
+  const uint32_t k_at = (uint32_t)(i * (D / 2) + g * (D / 8) + part * KWAVE * 4), v_at = (uint32_t)(8 * D + (i * 16 + 4 * g) * (D / 32) + part / 2 * 4);
+  const uint32_t ks_at = (uint32_t)(16 * D + i * (D / 32) + (D == 64 ? g / 2 : D == 128 ? g : 2 * g + part / 2));
   const uint32_t vs_at = (uint32_t)(16 * D + D / 2 + (D == 64 ? i / 8 : D == 128 ? i / 4 : i / 2) * 16 + 4 * g);
   auto look_up = [&](int n) __attribute__((always_inline)) {
     const int t = n * TT + kb * 16;
@@ -377,17 +394,20 @@ __global__ __launch_bounds__(kAttnRowWaves * 64, 2) void st_attn_rows_kernel(con
     raw.page = page;
     const char* at = block_of(T, raw.page < 0 ? 0 : raw.page, head, t, A::kBlock);
     if constexpr (KWAVE == 2) {
-      const u32x2 w = *(const u32x2*)(at + k_at), c = *(const u32x2*)(at + v_at);
-      raw.k[0] = w[0], raw.k[1] = w[1], raw.v[0] = c[0], raw.v[1] = c[1];
+      const u32x2 w = *(const u32x2*)(at + k_at);
+      raw.k[0] = w[0], raw.k[1] = w[1];
     } else {
       const u32x4 w = *(const u32x4*)(at + k_at);
       static_for<4>([&](auto X) { raw.k[decltype(X)::value] = w[decltype(X)::value]; });
-      if constexpr (SHARE == 1) {
-        const u32x4 c = *(const u32x4*)(at + v_at);
-        static_for<4>([&](auto X) { raw.v[decltype(X)::value] = c[decltype(X)::value]; });
-      } else {
-        static_for<4>([&](auto X) { raw.v[decltype(X)::value] = *(const uint32_t*)(at + v_at + 8 * decltype(X)::value); });
-      }
+    }
+    if constexpr (D == 64) {
+      const u32x2 c = *(const u32x2*)(at + v_at);
+      raw.v[0] = c[0], raw.v[1] = c[1];
+    } else if constexpr (D == 128) {
+      const u32x4 c = *(const u32x4*)(at + v_at);
+      static_for<4>([&](auto X) { raw.v[decltype(X)::value] = c[decltype(X)::value]; });
+    } else {
+      static_for<4>([&](auto X) { raw.v[decltype(X)::value] = *(const uint32_t*)(at + v_at + 8 * decltype(X)::value); });
     }
     raw.ks = *(const uint8_t*)(at + ks_at);
     raw.vs = *(const uint32_t*)(at + vs_at);
@@ -415,7 +435,7 @@ __global__ __launch_bounds__(kAttnRowWaves * 64, 2) void st_attn_rows_kernel(con
       static_for<4>([&](auto X) {
         constexpr int t = decltype(X)::value;
         if constexpr (D == 64) c[t] = widen<DT, t % 2 * 2 + e2>(raw.v[t / 2], vsc[t]);
-        else c[t] = widen<DT, e2>(raw.v[t], vsc[t]);
+        else c[t] = widen<DT, e2>(D == 128 ? raw.v[t] : raw.v[t] >> (part % 2 * 16), vsc[t]);
       });
       u32x2* to = (u32x2*)&frags[buf][KF + kb / 2 * NE + part * VWAVE + 2 * e2][lane] + kb % 2;
       to[0] = u32x2{__builtin_amdgcn_perm(c[1], c[0], 0x05040100u), __builtin_amdgcn_perm(c[3], c[2], 0x05040100u)};
@@ -426,7 +446,7 @@ __global__ __launch_bounds__(kAttnRowWaves * 64, 2) void st_attn_rows_kernel(con
   };
   const float scale = T.scale;
   // A tile's sub-steps read their fragments in order, keys then values, AHEAD of them before they are multiplied.
-  constexpr int AHEAD = 4, SF = 2 * KW + NE, SLOTS = TT / 32 * SF, EVERY = SLOTS / PIECES;
+  constexpr int AHEAD = D == 256 ? 8 : 4, SF = 2 * KW + NE, SLOTS = TT / 32 * SF, EVERY = 2;
   auto compute = [&](int n, int buf, int bad) __attribute__((always_inline)) {
     auto slot = [&](auto N) __attribute__((always_inline)) {
       constexpr int k = decltype(N)::value;
@@ -440,18 +460,17 @@ __global__ __launch_bounds__(kAttnRowWaves * 64, 2) void st_attn_rows_kernel(con
       u32x4 f[AHEAD];
       auto read = [&](auto F) __attribute__((always_inline)) {
         constexpr int k = decltype(F)::value;
-        if constexpr (k < SF) f[k % AHEAD] = frags[buf][k < 2 * KW ? 2 * u * KW + k : KF + u * NE + k - 2 * KW][lane];
+        if constexpr (k < SF) f[k % AHEAD] = frags[buf][k < 2 * KW ? 2 * u * KW + (R > 1 ? k : k % 2 * KW + k / 2) : KF + u * NE + k - 2 * KW][lane];
       };
       static_for<AHEAD>([&](auto F) { read(F); });
       f32x4 score[2][R];
-      static_for<2>([&](auto B) {
-        static_for<R>([&](auto J) { score[decltype(B)::value][decltype(J)::value] = f32x4{0.f, 0.f, 0.f, 0.f}; });
-        static_for<KW>([&](auto Q) __attribute__((always_inline)) {
-          constexpr int b = decltype(B)::value, w = decltype(Q)::value, k = b * KW + w;
-          static_for<R>([&](auto J) { score[b][decltype(J)::value] = A::Op::run(f[k % AHEAD], a.q[decltype(J)::value][w], score[b][decltype(J)::value]); });
-          read(std::integral_constant<int, k + AHEAD>{});
-          slot(std::integral_constant<int, u * SF + k>{});
-        });
+      static_for<2 * R>([&](auto J) { score[decltype(J)::value / R][decltype(J)::value % R] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+      static_for<2 * KW>([&](auto Q) __attribute__((always_inline)) {
+        // block after block, or, where a block's MFMAs would wait for one another, both in turn
+        constexpr int k = decltype(Q)::value, b = R > 1 ? k / KW : k % 2, w = R > 1 ? k % KW : k / 2;
+        static_for<R>([&](auto J) { score[b][decltype(J)::value] = A::Op::run(f[k % AHEAD], a.q[decltype(J)::value][w], score[b][decltype(J)::value]); });
+        read(std::integral_constant<int, k + AHEAD>{});
+        slot(std::integral_constant<int, u * SF + k>{});
       });
       u32x4 p[R];
       a.weigh(score, p, t0, mask, hid, T.window, scale, lane);
@@ -484,7 +503,7 @@ __global__ __launch_bounds__(kAttnRowWaves * 64, 2) void st_attn_rows_kernel(con
   static_for<R>([&](auto J) {
     constexpr int r = decltype(J)::value;
     const int row = row0 + r * 16 + i;
-    const float total = a.sum[r][0], inv = total == 0.f ? 0.f : 1.f / total;
+    const float total = a.row_sum(r), inv = total == 0.f ? 0.f : 1.f / total;
     if (row < rows) {
       static_for<4>([&](auto X) {
         constexpr int x = decltype(X)::value;
@@ -522,7 +541,7 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
   if (stretch >= active) return;
   const int begin = s_lo + stretch * T.chunk, end = stretch + 1 < active ? begin + T.chunk : s_lo + steps;
 
-  Attend<DT, D, R> a;
+  Attend<DT, D, R, false> a;
   a.clear();
   a.load_rows(T, S, head, row0, lane);
   a.template run<W>(T, seq, head, S.length, begin + wave, end, see.hi, see.all_lo, see.all_hi, lane);
@@ -541,7 +560,8 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
     ref[r] = top;
     const float down = __builtin_amdgcn_exp2f(a.m[r] - top);
     static_for<D / 16>([&](auto E) { a.acc[decltype(E)::value][r] *= down; });
-    if (g == 0) wave_l[wave][r * 16 + i] = a.sum[r][0] * down;
+    const float mine = a.row_sum(r) * down;
+    if (g == 0) wave_l[wave][r * 16 + i] = mine;
   });
   __syncthreads();
   if (tid < ROWS) {
@@ -606,7 +626,7 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
   __syncthreads();
   if (flag == 0u) return;
   if (tid < ROWS) {
-    float top = Attend<DT, D, R>::kNothing, total = 0.f;
+    float top = Attend<DT, D, R, false>::kNothing, total = 0.f;
     for (int s = 0; s < active; ++s) {
       const float ms = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rstat, (s * 2 * ROWS + tid) * 4, 0, kAuxDeviceCoherent));
       weight[s][tid] = ms;
@@ -745,7 +765,7 @@ static hipError_t launch_kind(int kind, unsigned blocks, void* stream, const Att
   switch (kind) {
     case kAttnTokens1: return launch(st_attn_tokens_kernel<DT, D, attn_blocks(kAttnTokens1, D)>, blocks, kAttnTokenWaves * 64, stream, table, items);
     case kAttnTokens2: return launch(st_attn_tokens_kernel<DT, D, attn_blocks(kAttnTokens2, D)>, blocks, kAttnTokenWaves * 64, stream, table, items);
-    case kAttnRows: return launch(st_attn_rows_kernel<DT, D, attn_blocks(kAttnRows, D)>, blocks, kAttnRowWaves * 64, stream, table, items);
+    case kAttnRows: return launch(st_attn_rows_kernel<DT, D, attn_blocks(kAttnRows, D)>, blocks, attn_row_waves(D) * 64, stream, table, items);
   }
   return hipErrorInvalidValue;
 }

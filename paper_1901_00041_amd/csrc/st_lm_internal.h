@@ -53,7 +53,8 @@ int launch_matmul(int dtype, int shape, const MatmulDev* table_dev, const Matmul
 // for the same rows, of which there are 16 R; kByRows: each wavefront takes 16 R rows of its own and all the tokens they see.
 constexpr int kAttnBlock = 16;           // tokens per cache block
 constexpr int kAttnStep = 32;            // tokens per step of a wavefront
-constexpr int kAttnTokenWaves = 8, kAttnRowWaves = 4;
+constexpr int kAttnTokenWaves = 8;
+constexpr int attn_row_waves(int dim) { return dim == 256 ? 8 : 4; }
 constexpr int kAttnMaxSplit = 64;
 constexpr int kAttnTokens1 = 0, kAttnTokens2 = 1, kAttnRows = 2, kNumAttnKinds = 3;
 // R of a kind: rows are as many as the registers hold beside their queries, scores and outputs
