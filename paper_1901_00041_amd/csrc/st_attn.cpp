@@ -93,6 +93,7 @@ int most_steps(const st_attn_desc& d) {      // that a row tile of single tokens
   if (d.window) tokens = std::min(tokens, (int64_t)d.window + d.max_new + kAttnStep);
   return cdiv(tokens, kAttnStep) + 1;
 }
+constexpr int kAttnMostSteps = 192, kAttnWholeSteps = 40;
 // Few rows: the tokens are divided among wavefronts and workgroups; else the rows are.
 int kind_of(const st_attn_desc& d) {
   const int rows = most_rows(d);
@@ -176,9 +177,12 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
       if (o.split_k > 0) {
         chunk = cdiv(steps, std::min(o.split_k, kAttnMaxSplit));
       } else {
-        // so many stretches that the chip is filled twice over, of at least two steps for each wavefront
-        const int want = std::max(1, std::min(kAttnMaxSplit, (int)std::ceil(2.0 * 2 * kNumCUs / tiles)));
-        chunk = std::max(2 * kAttnTokenWaves, cdiv(steps, want));
+        // A stretch on every compute unit: more of them only cost their set-up and their joining (one context of 131072, us with 24, 32, 64
+        // stretches: 35.3, 36.9, 42.9; 32 of 8000 with heads of 256, 128, 256, 512 workgroups: 43.1, 28.4, 36.3).  But none longer
+        // than 192 steps, or a few long sequences outlast the others (64 of up to 8192: 75.5 us in one stretch each, 66.9 in two),
+        // and short ones whole (a single sequence of 1000: 8.2 us whole, 9.1 in two; of 2000: 12.0 whole, 9.5 in four; of 4000: 19.9, 9.9 in eight).
+        const int want = std::max(1, std::min(kAttnMaxSplit, (int)std::ceil(kNumCUs / tiles)));
+        chunk = steps <= kAttnWholeSteps ? steps : std::max(2 * kAttnTokenWaves, cdiv(steps, std::max(want, std::min(kAttnMaxSplit, cdiv(steps, kAttnMostSteps)))));
       }
       T.chunk = chunk;
       T.split = cdiv(steps, chunk);

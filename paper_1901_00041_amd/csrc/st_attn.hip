@@ -625,38 +625,58 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
   }
   __syncthreads();
   if (flag == 0u) return;
+  // every stretch's maximum and sum of every row, all on their way at once
+  static_assert(sizeof(part) >= kAttnMaxSplit * ROWS * 4 && sizeof(part) >= THREADS * 16, "room for the sums, then for the groups' results");
+  float* sums = &part[0][0][0];
+  for (int at = tid; at < active * ROWS; at += THREADS) {
+    const int s = at / ROWS, row = at % ROWS;
+    weight[s][row] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rstat, (s * 2 * ROWS + row) * 4, 0, kAuxDeviceCoherent));
+    sums[at] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rstat, (s * 2 * ROWS + ROWS + row) * 4, 0, kAuxDeviceCoherent));
+  }
+  __syncthreads();
   if (tid < ROWS) {
     float top = Attend<DT, D, R, false>::kNothing, total = 0.f;
+    for (int s = 0; s < active; ++s) top = fmaxf(top, weight[s][tid]);
     for (int s = 0; s < active; ++s) {
-      const float ms = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rstat, (s * 2 * ROWS + tid) * 4, 0, kAuxDeviceCoherent));
-      weight[s][tid] = ms;
-      top = fmaxf(top, ms);
-    }
-    for (int s = 0; s < active; ++s) {
-      const float l = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rstat, (s * 2 * ROWS + ROWS + tid) * 4, 0, kAuxDeviceCoherent));
       const float w = __builtin_amdgcn_exp2f(weight[s][tid] - top);
       weight[s][tid] = w;
-      total += w * l;
+      total += w * sums[s * ROWS + tid];
     }
     inverse[tid] = total == 0.f ? 0.f : 1.f / total;
   }
   __syncthreads();
+  // Four outputs to a thread.  Where that leaves threads over, they share the stretches: group k takes stretches k, k + groups, ...
   const __amdgpu_buffer_rsrc_t rp = make_rsrc(parts, (uint32_t)T.split * ROWS * D * 4);
-  for (int at = tid; at < (row1 - row0) * (D / 4); at += THREADS) {
-    const int row = at / (D / 4), dim = at % (D / 4) * 4;
+  const int vectors = (row1 - row0) * (D / 4), groups = vectors < THREADS ? THREADS / vectors : 1, group = groups > 1 ? tid / vectors : 0;
+  for (int first = 0; first < vectors; first += THREADS) {
+    const int at = first + (groups > 1 ? tid - group * vectors : tid), row = at / (D / 4), dim = at % (D / 4) * 4;
+    const bool mine = at < vectors && group < groups;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < active; s0 += 8) {
-      f32x4 one[8];
+    if (mine) {
+      for (int s0 = group; s0 < active; s0 += 8 * groups) {
+        f32x4 one[8];
 #pragma unroll
-      for (int s = 0; s < 8; ++s)
-        one[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rp, (int)(s0 + s < active ? (uint32_t)(((s0 + s) * ROWS + row) * D + dim) * 4u : kInvalidOffset), 0, kAuxDeviceCoherent));
+        for (int k = 0; k < 8; ++k) {
+          const int s = s0 + k * groups;
+          one[k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rp, (int)(s < active ? (uint32_t)((s * ROWS + row) * D + dim) * 4u : kInvalidOffset), 0, kAuxDeviceCoherent));
+        }
 #pragma unroll
-      for (int s = 0; s < 8; ++s)
-        if (s0 + s < active) v += one[s] * weight[s0 + s][row];
+        for (int k = 0; k < 8; ++k)
+          if (s0 + k * groups < active) v += one[k] * weight[s0 + k * groups][row];
+      }
     }
-    const float f = inverse[row];
-    const float o[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
-    store_out<DT, 4>(T, S, head, row0 + row, dim, D, o);
+    if (groups > 1) {
+      f32x4* shared = (f32x4*)&part[0][0][0];
+      if (mine) shared[tid] = v;
+      __syncthreads();
+      if (tid < vectors)
+        for (int k = 1; k < groups; ++k) v += shared[k * vectors + tid];
+    }
+    if (mine && group == 0) {
+      const float f = inverse[row];
+      const float o[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
+      store_out<DT, 4>(T, S, head, row0 + row, dim, D, o);
+    }
   }
 }
 
