@@ -16,7 +16,7 @@ using namespace st;
 struct st_attn {
   std::vector<st_attn_desc> descs;
   std::vector<AttnDev> tenants;        // host mirror of the device table
-  struct Launch { int dtype, dim, kind; int64_t begin, count; };
+  struct Launch { int dtype, dim, kind; int64_t begin, count; };      // kind of a move: many new tokens
   std::vector<Launch> runs, moves;
   std::vector<AttnItem> items;         // of all launches, one after another
   bool can_append = true, can_read = true, can_run = true;      // every pointer is there that the call needs
@@ -98,6 +98,13 @@ constexpr int kAttnMostSteps = 192, kAttnWholeSteps = 40;
 int kind_of(const st_attn_desc& d) {
   const int rows = most_rows(d);
   return rows <= 16 ? kAttnTokens1 : rows <= 32 ? kAttnTokens2 : kAttnRows;
+}
+
+// Workgroups that move a sequence's new tokens.
+bool moves_many(const st_attn_desc& d) { return d.max_new >= kAttnBlock; }
+int move_parts(const st_attn_desc& d) {
+  const int64_t tokens = moves_many(d) ? cdiv(d.max_new, kAttnBlock) * kAttnBlock : d.max_new;
+  return cdiv(tokens * d.kv_heads, attn_move_count(d.head_dim) * (moves_many(d) ? kAttnMoveTurns : 1));
 }
 
 st_status upload(st_attn* p) {
@@ -188,8 +195,7 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
       T.split = cdiv(steps, chunk);
     }
     n_items += (int64_t)d.n_seqs * d.kv_heads * T.row_tiles * T.split;
-    const int64_t new_heads = (int64_t)(d.max_new >= 16 ? cdiv(d.max_new, 16) * 16 : d.max_new) * d.kv_heads;
-    const int64_t moves = (int64_t)d.n_seqs * cdiv(new_heads, attn_move_count(d.head_dim));
+    const int64_t moves = (int64_t)d.n_seqs * move_parts(d);
     if (n_items >= ((int64_t)1 << 28) || moves >= ((int64_t)1 << 28)) return fail(ST_ERR_UNSUPPORTED, "more than 2^28 workgroups");
   }
   for (int dtype : {ST_DT_BF16, ST_DT_F16})
@@ -213,18 +219,18 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
     }
   p->totals.launches = (int32_t)p->runs.size();
   for (int dtype : {ST_DT_BF16, ST_DT_F16})
-    for (int dim : {64, 128, 256}) {
-      const int64_t begin = (int64_t)p->items.size();
-      for (int t = 0; t < n; ++t) {
-        const st_attn_desc& d = descs[t];
-        if (d.dtype != dtype || d.head_dim != dim || d.n_seqs == 0 || d.max_tokens == 0) continue;
-        const int64_t new_heads = (int64_t)(d.max_new >= 16 ? cdiv(d.max_new, 16) * 16 : d.max_new) * d.kv_heads;
-        const int parts = cdiv(new_heads, attn_move_count(dim));
-        for (int s = 0; s < d.n_seqs; ++s)
-          for (int part = 0; part < parts; ++part) p->items.push_back({(uint32_t)t, (uint32_t)s, 0u, (uint32_t)part});
+    for (int dim : {64, 128, 256})
+      for (int many = 0; many < 2; ++many) {
+        const int64_t begin = (int64_t)p->items.size();
+        for (int t = 0; t < n; ++t) {
+          const st_attn_desc& d = descs[t];
+          if (d.dtype != dtype || d.head_dim != dim || moves_many(d) != (many != 0) || d.n_seqs == 0 || d.max_tokens == 0) continue;
+          const int parts = move_parts(d);
+          for (int s = 0; s < d.n_seqs; ++s)
+            for (int part = 0; part < parts; ++part) p->items.push_back({(uint32_t)t, (uint32_t)s, 0u, (uint32_t)part});
+        }
+        if ((int64_t)p->items.size() > begin) p->moves.push_back({dtype, dim, many, begin, (int64_t)p->items.size() - begin});
       }
-      if ((int64_t)p->items.size() > begin) p->moves.push_back({dtype, dim, 0, begin, (int64_t)p->items.size() - begin});
-    }
   return upload(p);
 }
 
@@ -242,7 +248,7 @@ st_status move(const st_attn* plan, bool read, void* hip_stream) {
   OnDevice on(plan->device);
   ST_HIP(on.error);
   for (const st_attn::Launch& l : plan->moves)
-    ST_HIP((hipError_t)launch_attn_move(read, l.dtype, l.dim, plan->d_tenants, plan->d_items + l.begin, l.count, hip_stream));
+    ST_HIP((hipError_t)launch_attn_move(read, l.kind != 0, l.dtype, l.dim, plan->d_tenants, plan->d_items + l.begin, l.count, hip_stream));
   return ST_OK;
 }
 

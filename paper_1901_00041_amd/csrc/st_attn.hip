@@ -681,102 +681,115 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
 }
 
 // ---- into the cache and out of it ---------------------------------------------------------------------------------------
-// dim / 8 lanes to a token's head: each has eight elements of the key and of the value.  With many new tokens 16 of them, of one head,
-// lie side by side, as they do in a block.
+// dim / 8 lanes to a token's head: each has eight elements of the key and of the value.  A wavefront's instructions are what a prompt costs
+// (13 000 tokens of eight heads of 128, 68 MB, in 23 us with 430 of them for each 2 KB; 18.3 now), so a workgroup takes kAttnMoveTurns
+// stretches of them, 16 tokens of a head side by side, and looks at values as integers: of a type's absolute values the larger one has the larger bits.
+__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t in_quad(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true); }
+// Eight elements' codes and their group's scale; finite: all of the group's are.
 template <int DT>
-__device__ __forceinline__ void encode8(const u32x4 in, int lane, uint32_t& codes, uint32_t& scale, bool& finite) {
-  float v[8], most = 0.f;
-  finite = true;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    v[e] = unpack16<DT>(in[e / 2], e & 1);
-    finite &= __builtin_fabsf(v[e]) < __builtin_inff();
-    most = fmaxf(most, __builtin_fabsf(v[e]));
-  }
-  most = fmaxf(most, __shfl_xor(most, 1));      // four lanes to a group of 32
-  most = fmaxf(most, __shfl_xor(most, 2));
-  const uint32_t bits = __builtin_bit_cast(uint32_t, most);
+__device__ __forceinline__ void encode8(const u32x4 in, uint32_t& codes, uint32_t& scale, bool& finite) {
+  const uint32_t all = 0x7fff7fffu;
+  uint32_t m = max16(max16(in[0] & all, in[1] & all), max16(in[2] & all, in[3] & all));
+  m = max16(m, m >> 16) & 0xffffu;
+  m = max16(m, in_quad<0xB1>(m));      // four lanes to a group of 32
+  m = max16(m, in_quad<0x4E>(m));
+  finite = m < (DT == ST_DT_BF16 ? 0x7f80u : 0x7c00u);
+  const uint32_t bits = __builtin_bit_cast(uint32_t, unpack16<DT>(m, 0));
   int e = (int)(bits >> 23) - 2 + ((bits & 0x7fffffu) > 0x400000u ? 1 : 0);
   e = e < 1 ? 1 : e > 252 ? 252 : e;
   scale = (uint32_t)e;
   const float f = __builtin_bit_cast(float, scale << 23);
   uint32_t c = 0;
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], f, 0);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], f, 1);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], f, 2);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], f, 3);
+  static_for<4>([&](auto X) {
+    constexpr int x = decltype(X)::value;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, unpack16<DT>(in[x], 0), unpack16<DT>(in[x], 1), f, x);
+  });
   codes = c;
 }
 
-template <int DT, int D, bool READ>
+template <int DT, int D, bool READ, int TURNS>
 __global__ __launch_bounds__(256) void st_attn_move_kernel(const AttnDev* table, const AttnItem* items) {
-  constexpr int LPT = D / 8, kBlock = attn_block_bytes(D);
+  constexpr int LPT = D / 8, TH = attn_move_count(D), kBlock = attn_block_bytes(D);
   const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
   ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
-  const int seq = (int)ci.seq, lane = (int)threadIdx.x & 63, c = (int)threadIdx.x % LPT;
+  const int seq = (int)ci.seq, tid = (int)threadIdx.x, lane = tid & 63, c = tid % LPT, slot = tid / LPT;
   const Seq S = sequence(T, seq);
-  const int th = (int)ci.part * attn_move_count(D) + (int)threadIdx.x / LPT;
-  int j, head;
-  if (T.max_new >= 16) {
-    const int group = th / 16;
-    head = group % T.kv_heads;
-    j = group / T.kv_heads * 16 + th % 16;
-  } else {
-    j = th / T.kv_heads;
-    head = th - j * T.kv_heads;
-  }
-  const bool real = j < S.n;
-  const int pos = S.before + j;
-  int page = -1;
-  if (real && pos >= 0) {
-    const int p = T.table[(int64_t)seq * T.table_pages + (pos >> T.page_shift)];
-    if ((uint32_t)p < (uint32_t)T.n_pages) page = p;
-    else if (c == 0) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_PAGE);
-  }
-  const int t = pos & 15;
-  char* at = const_cast<char*>(block_of(T, page < 0 ? 0 : page, head, pos, kBlock));
-  char *kp = at + t * (D / 2) + c * 4, *ks = at + 16 * D + t * (D / 32) + c / 4, *vs = at + 16 * D + D / 2 + (c / 4) * 16 + t;
-  char* vp = at + 8 * D + (D == 64 ? (2 * c * 16 + t) * 2 : D == 128 ? (c * 16 + t) * 4 : (c / 2 * 16 + t) * 8 + c % 2 * 4);
-  const int64_t row = S.first + (real ? j : 0);
-  if constexpr (!READ) {
-    u32x4 k = {0u, 0u, 0u, 0u}, v = k;
-    if (page >= 0) {
-      k = *(const u32x4_any*)((const uint16_t*)T.k + row * T.ldk + head * D + c * 8);
-      v = *(const u32x4_any*)((const uint16_t*)T.v + row * T.ldv + head * D + c * 8);
-    }
-    uint32_t kc, kscale, vc, vscale;
-    bool kfin, vfin;
-    encode8<DT>(k, lane, kc, kscale, kfin);
-    encode8<DT>(v, lane, vc, vscale, vfin);
-    const uint64_t odd = __ballot(!(kfin && vfin)) >> (lane & ~(LPT - 1));
-    if ((odd & (((uint64_t)1 << LPT) - 1)) != 0) kc = vc = 0u, kscale = 255u, vscale = 1u;
-    if (page < 0) return;
-    *(uint32_t*)kp = kc;
-    if constexpr (D == 64) {
-      *(uint16_t*)vp = (uint16_t)vc;
-      *(uint16_t*)(vp + 32) = (uint16_t)(vc >> 16);
+  const int32_t* row_of_table = T.table + (int64_t)seq * T.table_pages;
+  const int kv = T.kv_heads, shift = T.page_shift;
+  int j[TURNS], head[TURNS], page[TURNS];
+  u32x4 k[TURNS], v[TURNS];
+  static_for<TURNS>([&](auto N) {
+    constexpr int n = decltype(N)::value;
+    const int th = ((int)ci.part * TURNS + n) * TH + slot;
+    if constexpr (TURNS > 1) {            // 16 tokens of a head, then those of the next: a wavefront has tokens of one head
+      const int group = __builtin_amdgcn_readfirstlane(th / 16);
+      head[n] = group % kv;
+      j[n] = group / kv * 16 + th % 16;
     } else {
-      *(uint32_t*)vp = vc;
+      j[n] = th / kv;
+      head[n] = th - j[n] * kv;
     }
-    if (c % 4 == 0) {
-      *ks = (char)kscale;
-      *vs = (char)vscale;
+    const bool real = j[n] < S.n;
+    const int pos = S.before + j[n];
+    page[n] = real && pos >= 0 ? row_of_table[pos >> shift] : -1;
+    k[n] = v[n] = u32x4{0u, 0u, 0u, 0u};
+    if (!READ && real) {
+      const int64_t row = S.first + j[n];
+      k[n] = *(const u32x4_any*)((const uint16_t*)T.k + row * T.ldk + head[n] * D + c * 8);
+      v[n] = *(const u32x4_any*)((const uint16_t*)T.v + row * T.ldv + head[n] * D + c * 8);
     }
-  } else {
-    if (!real) return;
-    u32x4 k = {0u, 0u, 0u, 0u}, v = k;
-    if (page >= 0) {
-      const uint32_t kc = *(const uint32_t*)kp;
-      uint32_t vc;
-      if constexpr (D == 64) vc = *(const uint16_t*)vp | (uint32_t)*(const uint16_t*)(vp + 32) << 16;
-      else vc = *(const uint32_t*)vp;
-      const float kf = key_scale<DT>(*(const uint8_t*)ks), vf = value_scale<DT>(*(const uint8_t*)vs);
-      k = u32x4{widen<DT, 0>(kc, kf), widen<DT, 1>(kc, kf), widen<DT, 2>(kc, kf), widen<DT, 3>(kc, kf)};
-      v = u32x4{widen<DT, 0>(vc, vf), widen<DT, 1>(vc, vf), widen<DT, 2>(vc, vf), widen<DT, 3>(vc, vf)};
+  });
+  static_for<TURNS>([&](auto N) {
+    constexpr int n = decltype(N)::value;
+    const bool real = j[n] < S.n;
+    const int pos = S.before + j[n], t = pos & 15;
+    if (real && pos >= 0 && (uint32_t)page[n] >= (uint32_t)T.n_pages) {
+      page[n] = -1;
+      if (c == 0) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_PAGE);
     }
-    *(u32x4_any*)((uint16_t*)T.k_out + row * T.ldk + head * D + c * 8) = k;
-    *(u32x4_any*)((uint16_t*)T.v_out + row * T.ldv + head * D + c * 8) = v;
-  }
+    char* at = const_cast<char*>(block_of(T, page[n] < 0 ? 0 : page[n], head[n], pos, kBlock));
+    char *kp = at + t * (D / 2) + c * 4, *ks = at + 16 * D + t * (D / 32) + c / 4, *vs = at + 16 * D + D / 2 + (c / 4) * 16 + t;
+    char* vp = at + 8 * D + (D == 64 ? (2 * c * 16 + t) * 2 : D == 128 ? (c * 16 + t) * 4 : (c / 2 * 16 + t) * 8 + c % 2 * 4);
+    if constexpr (!READ) {
+      uint32_t kc, kscale, vc, vscale;
+      bool kfin, vfin;
+      encode8<DT>(k[n], kc, kscale, kfin);
+      encode8<DT>(v[n], vc, vscale, vfin);
+      const uint64_t odd = __ballot(!(kfin && vfin));
+      if (odd != 0 && ((odd >> (lane & ~(LPT - 1))) & (((uint64_t)1 << LPT) - 1)) != 0) kc = vc = 0u, kscale = 255u, vscale = 1u;
+      if (page[n] >= 0) {
+        *(uint32_t*)kp = kc;
+        if constexpr (D == 64) {
+          *(uint16_t*)vp = (uint16_t)vc;
+          *(uint16_t*)(vp + 32) = (uint16_t)(vc >> 16);
+        } else {
+          *(uint32_t*)vp = vc;
+        }
+        if (c % 4 == 0) {
+          *ks = (char)kscale;
+          *vs = (char)vscale;
+        }
+      }
+    } else if (real) {
+      if (page[n] >= 0) {
+        const uint32_t kc = *(const uint32_t*)kp;
+        uint32_t vc;
+        if constexpr (D == 64) vc = *(const uint16_t*)vp | (uint32_t)*(const uint16_t*)(vp + 32) << 16;
+        else vc = *(const uint32_t*)vp;
+        const float kf = key_scale<DT>(*(const uint8_t*)ks), vf = value_scale<DT>(*(const uint8_t*)vs);
+        k[n] = u32x4{widen<DT, 0>(kc, kf), widen<DT, 1>(kc, kf), widen<DT, 2>(kc, kf), widen<DT, 3>(kc, kf)};
+        v[n] = u32x4{widen<DT, 0>(vc, vf), widen<DT, 1>(vc, vf), widen<DT, 2>(vc, vf), widen<DT, 3>(vc, vf)};
+      }
+      const int64_t row = S.first + j[n];
+      *(u32x4_any*)((uint16_t*)T.k_out + row * T.ldk + head[n] * D + c * 8) = k[n];
+      *(u32x4_any*)((uint16_t*)T.v_out + row * T.ldv + head[n] * D + c * 8) = v[n];
+    }
+  });
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------------
@@ -800,16 +813,20 @@ int launch_attn(int dtype, int dim, int kind, const AttnDev* table_dev, const At
                                    : launch_dim<ST_DT_F16>(dim, kind, (unsigned)n_items, stream, table_dev, items_dev));
 }
 
-template <int DT, bool READ>
+template <int DT, bool READ, int TURNS>
 static hipError_t launch_move(int dim, unsigned blocks, void* stream, const AttnDev* table, const AttnItem* items) {
-  auto kernel = dim == 64 ? st_attn_move_kernel<DT, 64, READ> : dim == 128 ? st_attn_move_kernel<DT, 128, READ> : st_attn_move_kernel<DT, 256, READ>;
+  auto kernel = dim == 64 ? st_attn_move_kernel<DT, 64, READ, TURNS> : dim == 128 ? st_attn_move_kernel<DT, 128, READ, TURNS> : st_attn_move_kernel<DT, 256, READ, TURNS>;
   return launch(kernel, blocks, 256, stream, table, items);
 }
-int launch_attn_move(bool read, int dtype, int dim, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream) {
+template <int DT>
+static hipError_t launch_move_any(bool read, bool many, int dim, unsigned blocks, void* stream, const AttnDev* table, const AttnItem* items) {
+  const auto run = read ? (many ? launch_move<DT, true, kAttnMoveTurns> : launch_move<DT, true, 1>) : (many ? launch_move<DT, false, kAttnMoveTurns> : launch_move<DT, false, 1>);
+  return run(dim, blocks, stream, table, items);
+}
+int launch_attn_move(bool read, bool many, int dtype, int dim, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream) {
   if (n_items <= 0) return 0;
-  const auto run = dtype == ST_DT_BF16 ? (read ? launch_move<ST_DT_BF16, true> : launch_move<ST_DT_BF16, false>)
-                                       : (read ? launch_move<ST_DT_F16, true> : launch_move<ST_DT_F16, false>);
-  return (int)run(dim, (unsigned)n_items, stream, table_dev, items_dev);
+  return (int)(dtype == ST_DT_BF16 ? launch_move_any<ST_DT_BF16>(read, many, dim, (unsigned)n_items, stream, table_dev, items_dev)
+                                   : launch_move_any<ST_DT_F16>(read, many, dim, (unsigned)n_items, stream, table_dev, items_dev));
 }
 
 }  // namespace st

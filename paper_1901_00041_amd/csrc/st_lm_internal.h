@@ -92,9 +92,10 @@ static_assert(sizeof(AttnDev) == 208, "a multiple of 16 bytes for launch_poke");
 struct AttnItem { uint32_t tenant, seq, head, part; };   // part: row tile * split + stretch, or the stretch of new tokens
 
 int launch_attn(int dtype, int dim, int kind, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream);
-// new tokens into the cache, or (read) out of it; part: the stretch of attn_move_count() of a sequence's new tokens x key heads
-int launch_attn_move(bool read, int dtype, int dim, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream);
-// token-heads that a workgroup of these moves
+// New tokens into the cache, or (read) out of it; part: the stretch of attn_move_count() of a sequence's new tokens x key heads, or (many: for
+// tenants that may have 16 new tokens or more) of kAttnMoveTurns times as many.
+int launch_attn_move(bool read, bool many, int dtype, int dim, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream);
+constexpr int kAttnMoveTurns = 2;
 constexpr int attn_move_count(int dim) { return 256 / (dim / 8); }
 
 }  // namespace st
