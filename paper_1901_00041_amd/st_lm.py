@@ -93,7 +93,7 @@ class AttnPlan(_Owned):
 def _run(name: str, plan: _Owned, stream) -> None:
     # the stream and the status are looked at here: a decoding step makes several of these calls, each a few microseconds long
     try:
-        st = getattr(lib(), name)(plan.handle, stream if stream is None or type(stream) is int else stream.cuda_stream)
+        st = getattr(sc._lib if _bound else lib(), name)(plan.handle, stream if stream is None or type(stream) is int else stream.cuda_stream)
     except (AttributeError, ctypes.ArgumentError):
         st = getattr(lib(), name)(plan.handle, _stream(stream))
     if st != sc.ST_OK:
