@@ -71,8 +71,9 @@ st_status validate_pointers(const st_attn_desc& d, const st_attn_desc& p, int t,
   const Span q = rows(p.q, d.heads, d.ldq), out = rows(p.out, d.heads, d.ldo), k_out = rows(p.k_out, d.kv_heads, d.ldk), v_out = rows(p.v_out, d.kv_heads, d.ldv);
   const int64_t pool_bytes = d.n_pages * page_bytes(d);
   const Span pool = {(uintptr_t)p.pages, p.pages && pool_bytes ? 1 : 0, pool_bytes, pool_bytes};
-  if (overlap(out, q) || overlap(out, pool) || overlap(k_out, pool) || overlap(v_out, pool) || overlap(k_out, v_out))
-    return fail(ST_ERR_INVALID_ARG, "tenant %d: outputs must not overlap q, the pages or each other", t);
+  const Span k = rows(p.k, d.kv_heads, d.ldk), v = rows(p.v, d.kv_heads, d.ldv);
+  if (overlap(out, q) || overlap(out, pool) || overlap(k_out, pool) || overlap(v_out, pool) || overlap(k_out, v_out) || overlap(k, pool) || overlap(v, pool))
+    return fail(ST_ERR_INVALID_ARG, "tenant %d: outputs must not overlap q, the pages or each other, nor k and v the pages", t);
   if (idle) return ST_OK;
   const bool tables = p.table && p.first && p.length && (p.pages || d.n_pages == 0);
   *append &= tables && p.k && p.v;
@@ -102,10 +103,23 @@ int kind_of(const st_attn_desc& d) {
 
 // Workgroups that move a sequence's new tokens.
 bool moves_many(const st_attn_desc& d) { return d.max_new >= kAttnBlock; }
-int move_parts(const st_attn_desc& d) {
-  const int64_t tokens = moves_many(d) ? cdiv(d.max_new, kAttnBlock) * kAttnBlock : d.max_new;
-  return cdiv(tokens * d.kv_heads, attn_move_count(d.head_dim) * (moves_many(d) ? kAttnMoveTurns : 1));
+int move_unit(const st_attn_desc& d) { return attn_move_count(d.head_dim) * (moves_many(d) ? kAttnMoveTurns : 1); }      // tokens x key heads of one
+int64_t move_parts(const st_attn_desc& d) {
+  const int64_t tokens = moves_many(d) ? ((int64_t)d.max_new + kAttnBlock - 1) / kAttnBlock * kAttnBlock : d.max_new;
+  return (tokens * d.kv_heads + move_unit(d) - 1) / move_unit(d);
 }
+// How many parts all sequences' max_tokens rows can make together.  Where listing what each sequence can have alone takes more than kAttnLoose
+// times as many, the parts' sequences are looked up instead: a workgroup without work holds its place for some two microseconds, a look-up
+// costs every one that has some as much.  Append and attention in us, listed and looked up: 256 sequences of 32 new tokens and some 500 in
+// all, max_new and max_tokens 8192 (107 times as many) 634 and 423, 12.7 and 148; 16 of 128, 2048 (12 times) 12.8 and 40.5, 5.1 and
+// 36.9; 4 of 1024, 4096 (4 times) 8.7 and 66.5, 6.2 and 71.3.
+constexpr int kAttnLoose = 4;
+int64_t all_moves(const st_attn_desc& d) { return (int64_t)d.max_tokens * d.kv_heads / move_unit(d) + (int64_t)d.n_seqs * ((kAttnBlock - 1) * (int64_t)d.kv_heads / move_unit(d) + 2); }
+bool find_moves(const st_attn_desc& d) { return moves_many(d) && d.n_seqs * move_parts(d) > kAttnLoose * all_moves(d); }
+int64_t all_row_tiles(const st_attn_desc& d) {
+  return (int64_t)d.max_tokens * (d.heads / d.kv_heads) / (attn_row_waves(d.head_dim) * 16 * attn_blocks(kAttnRows, d.head_dim)) + d.n_seqs;
+}
+bool find_rows(const st_attn_desc& d, int64_t row_tiles) { return kind_of(d) == kAttnRows && d.n_seqs * row_tiles > kAttnLoose * all_row_tiles(d); }
 
 st_status upload(st_attn* p) {
   const size_t n = p->tenants.size();
@@ -166,14 +180,14 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
     T.table_pages = d.table_pages; T.window = d.window; T.causal = (d.flags & ST_ATTN_CAUSAL) != 0;
     // hidden tokens get the score -inf, which has to stay that under the scale: a negative one changes the queries' signs instead, and one of
     // 0, or so small, counts as 2^-100, under which all finite scores are equal, too
-    T.scale = std::max(std::fabs(d.scale) * 1.44269504088896340736f, 7.888609e-31f);
+    T.scale = std::min(std::max(std::fabs(d.scale) * 1.44269504088896340736f, 7.888609e-31f), 3.0e38f);
     T.flip = d.scale < 0 ? 0x80008000u : 0u;
     T.row_tiles = cdiv(most_rows(d), (kind == kAttnRows ? attn_row_waves(d.head_dim) : 1) * 16 * attn_blocks(kind, d.head_dim));
     T.split = 1;
     T.chunk = 1 << 30;
     if (d.max_tokens > 0 && kind != kAttnRows) tiles += (double)d.n_seqs * d.kv_heads * T.row_tiles;
   }
-  int64_t n_items = 0;
+  int64_t n_items = 0, n_moves = 0;
   for (int t = 0; t < n; ++t) {
     const st_attn_desc& d = descs[t];
     AttnDev& T = p->tenants[t];
@@ -194,9 +208,9 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
       T.chunk = chunk;
       T.split = cdiv(steps, chunk);
     }
-    n_items += (int64_t)d.n_seqs * d.kv_heads * T.row_tiles * T.split;
-    const int64_t moves = (int64_t)d.n_seqs * move_parts(d);
-    if (n_items >= ((int64_t)1 << 28) || moves >= ((int64_t)1 << 28)) return fail(ST_ERR_UNSUPPORTED, "more than 2^28 workgroups");
+    n_items += find_rows(d, T.row_tiles) ? all_row_tiles(d) * d.kv_heads + 1 : (int64_t)d.n_seqs * d.kv_heads * T.row_tiles * T.split;
+    n_moves += find_moves(d) ? all_moves(d) + 1 : d.n_seqs * move_parts(d);
+    if (n_items >= kMostWorkgroups || n_moves >= kMostWorkgroups) return fail(ST_ERR_UNSUPPORTED, "more than 2^23 workgroups");
   }
   for (int dtype : {ST_DT_BF16, ST_DT_F16})
     for (int dim : {64, 128, 256}) {
@@ -206,6 +220,12 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
           const st_attn_desc& d = descs[t];
           const AttnDev& T = p->tenants[t];
           if (d.dtype != dtype || d.head_dim != dim || kind_of(d) != kind || d.n_seqs == 0 || d.max_tokens == 0) continue;
+          if (find_rows(d, T.row_tiles)) {
+            p->items.push_back({(uint32_t)t, kAttnCheck, 0u, 0u});
+            for (int64_t part = 0; part < all_row_tiles(d); ++part)
+              for (int h = 0; h < d.kv_heads; ++h) p->items.push_back({(uint32_t)t, kAttnFind, (uint32_t)h, (uint32_t)part});
+            continue;
+          }
           // a sequence's last rows see most; a key head's row tiles stay on one XCD where the heads divide well
           const int parts = T.row_tiles * T.split;
           for (int part = 0; part < parts; ++part)
@@ -225,7 +245,12 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
         for (int t = 0; t < n; ++t) {
           const st_attn_desc& d = descs[t];
           if (d.dtype != dtype || d.head_dim != dim || moves_many(d) != (many != 0) || d.n_seqs == 0 || d.max_tokens == 0) continue;
-          const int parts = move_parts(d);
+          if (find_moves(d)) {
+            p->items.push_back({(uint32_t)t, kAttnCheck, 0u, 0u});
+            for (int64_t part = 0; part < all_moves(d); ++part) p->items.push_back({(uint32_t)t, kAttnFind, 0u, (uint32_t)part});
+            continue;
+          }
+          const int parts = (int)move_parts(d);
           for (int s = 0; s < d.n_seqs; ++s)
             for (int part = 0; part < parts; ++part) p->items.push_back({(uint32_t)t, (uint32_t)s, 0u, (uint32_t)part});
         }

@@ -32,14 +32,45 @@ struct Seq {
   int length;     // tokens in the cache
   int before;     // position of the first new token (negative: there are more new tokens than tokens)
 };
-__device__ __forceinline__ Seq sequence(ConstAttn& T, int seq) {
+__device__ __forceinline__ Seq sequence(ConstAttn& T, int seq, bool reports) {      // reports: this thread, what was held
   const int a = ((ConstInt*)T.first)[seq], b = ((ConstInt*)T.first)[seq + 1], len = ((ConstInt*)T.length)[seq];
   const int64_t cap = (int64_t)T.table_pages << T.page_shift;
   const int f0 = a < 0 ? 0 : a > T.max_tokens ? T.max_tokens : a, f1 = b < f0 ? f0 : b > T.max_tokens ? T.max_tokens : b;
   const int length = len < 0 ? 0 : len > cap ? (int)cap : len;
   const int all = f1 - f0, n = all < T.max_new ? all : T.max_new;
-  if (threadIdx.x == 0 && (f0 != a || f1 != b || length != len || n != all || all > length)) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_LENGTH);
+  if (reports && (f0 != a || f1 != b || length != len || n != all || all > length)) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_LENGTH);
   return {f0, n, length, length - all};
+}
+// Where max_new allows far more work than max_tokens, items are not listed for each sequence, which leaves most of them without any, but
+// as many as there can be at most in all (kAttnFind): the part-th of all parts belongs to the sequence that is found here, 64 sequences at a
+// time, and is that sequence's part-th then.  parts(n): of a sequence with n new tokens.  One more item (kAttnCheck) looks at every sequence's numbers.
+template <class Parts>
+__device__ __forceinline__ bool find_sequence(ConstAttn& T, uint32_t item_seq, int& seq, int& part, Parts&& parts) {
+  seq = (int)item_seq;
+  if (__builtin_expect(item_seq < kAttnFind, 1)) return true;
+  const int lane = (int)threadIdx.x & 63;
+  if (item_seq == kAttnCheck) {
+    for (int s = (int)threadIdx.x; s < T.n_seqs; s += (int)blockDim.x) (void)sequence(T, s, true);
+    return false;
+  }
+  for (int s0 = 0, before = 0; s0 < T.n_seqs; s0 += 64) {      // before <= part: no sum passes 2^31
+    int up_to = s0 + lane < T.n_seqs ? parts(sequence(T, s0 + lane, false).n) : 0;
+    up_to = up_to < 1 << 24 ? up_to : 1 << 24;
+    const int mine = up_to;
+    for (int k = 1; k < 64; k *= 2) {
+      const int below = __shfl_up(up_to, k);
+      up_to += lane >= k ? below : 0;
+    }
+    const uint64_t behind = __ballot(before + up_to > part);
+    if (behind != 0) {
+      const int at = __builtin_ctzll(behind);
+      seq = s0 + at;
+      part -= before + __builtin_amdgcn_readlane(up_to - mine, at);
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(up_to, 63);
+  }
+  return false;
 }
 // A stretch of a sequence's table, an entry a lane, so that looking a page up costs no trip to memory (nor a scalar load, which would
 // make every wait for LDS a wait for all of it).
@@ -295,17 +326,17 @@ struct Attend {
     });
   }
 
-  // Steps begin, begin + STRIDE, ... before end; `last`: the last token that any row sees; tokens [all_lo, all_hi] are seen by all rows.
+  // Steps begin, begin + STRIDE, ... before end; `first`, `last`: the first and last tokens that any row sees; tokens [all_lo, all_hi] are seen by all rows.
   template <int STRIDE>
-  __device__ __forceinline__ void run(ConstAttn& T, int seq, int head, int length, int begin, int end, int last, int all_lo, int all_hi, int lane) {
+  __device__ __forceinline__ void run(ConstAttn& T, int seq, int head, int length, int begin, int end, int first, int last, int all_lo, int all_hi, int lane) {
     if (begin >= end) return;
     const float scale = T.scale;
     const int final_step = end - 1;
     auto held = [&](int s) { return s < final_step ? s : final_step; };      // what is fetched ahead stays inside
     int bad = 0;
     auto compute = [&](const Raw& raw, int s) __attribute__((always_inline)) {
-      bad |= raw.bad;
       const int t = s * kAttnStep;
+      bad |= t + 16 <= first ? raw.bad & 2 : raw.bad;      // a page before all windows may be gone
       step(raw, s, length, T.window, scale, lane, !(t >= all_lo && t + kAttnStep - 1 <= all_hi && raw.bad == 0));
     };
     Table table(T, seq, begin * kAttnStep, last, lane);
@@ -334,7 +365,10 @@ __device__ __forceinline__ Seen seen_by(ConstAttn& T, const Seq& S, int row0, in
   s.all_hi = T.causal ? p0 : S.length - 1;
   s.lo = T.window && p0 - T.window + 1 > 0 ? p0 - T.window + 1 : 0;
   s.all_lo = T.window && p1 - T.window + 1 > 0 ? p1 - T.window + 1 : 0;
-  if (T.n_pages == 0) s.hi = -1;
+  if (T.n_pages == 0) {
+    if (s.hi >= 0 && threadIdx.x == 0) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_PAGE);
+    s.hi = -1;
+  }
   return s;
 }
 
@@ -363,12 +397,16 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
   __shared__ __align__(16) int hidden[2][BLOCKS];
   const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
   ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
-  const int seq = (int)ci.seq, head = (int)ci.head;
+  constexpr int ROWS = W * 16 * R;
+  int seq, part_of = (int)ci.part;
+  const int group = T.group;
+  if (!find_sequence(T, ci.seq, seq, part_of, [group](int n) { return (n * group + ROWS - 1) / ROWS; })) return;
+  const int head = (int)ci.head;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
-  const Seq S = sequence(T, seq);
-  const int rows = S.n * T.group, block0 = (int)ci.part * W * 16 * R, row0 = block0 + wave * 16 * R;
-  if (block0 >= rows) return;
-  const int block1 = block0 + W * 16 * R < rows ? block0 + W * 16 * R : rows;
+  const Seq S = sequence(T, seq, threadIdx.x == 0);
+  const int rows = S.n * group, block0 = (ci.seq == kAttnFind ? (rows - 1) / ROWS - part_of : part_of) * ROWS, row0 = block0 + wave * 16 * R;
+  if (block0 >= rows || block0 < 0) return;
+  const int block1 = block0 + ROWS < rows ? block0 + ROWS : rows;
   const int row1 = row0 + 16 * R < rows ? row0 + 16 * R : rows;
   const Seen all = seen_by(T, S, block0, block1);
   Seen see = seen_by(T, S, row0 < rows ? row0 : block0, row0 < rows ? row1 : block1);
@@ -446,7 +484,7 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
   };
   const float scale = T.scale;
   // A tile's sub-steps read their fragments in order, keys then values, AHEAD of them before they are multiplied.
-  constexpr int AHEAD = D == 256 ? 8 : 4, SF = 2 * KW + NE, SLOTS = TT / 32 * SF, EVERY = 2;
+  constexpr int AHEAD = D == 256 ? 8 : 4, SF = 2 * KW + NE, EVERY = 2;
   auto compute = [&](int n, int buf, int bad) __attribute__((always_inline)) {
     auto slot = [&](auto N) __attribute__((always_inline)) {
       constexpr int k = decltype(N)::value;
@@ -494,7 +532,9 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
       int bad = 0;
       static_for<BLOCKS>([&](auto B) { bad |= hidden[buf][decltype(B)::value] << decltype(B)::value; });
       bad = __builtin_amdgcn_readfirstlane(bad);
-      bad_pages |= bad & ((2 << ((all.hi - n * TT) / 16 < BLOCKS ? (all.hi - n * TT) / 16 : BLOCKS - 1)) - 1);      // of blocks up to the last token
+      // of blocks from the first token to the last that somebody sees: pages before all windows may be gone
+      const int from = all.lo - n * TT > 0 ? (all.lo - n * TT) / 16 : 0, to = (all.hi - n * TT) / 16 < BLOCKS ? (all.hi - n * TT) / 16 : BLOCKS - 1;
+      bad_pages |= bad & ((2 << to) - (1 << from));
       compute(n, buf, bad);      // also where the wavefront's rows see none of it, a few tiles at a sequence's ends: one path keeps the sums in place
       __syncthreads();
     }
@@ -531,7 +571,7 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
   ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
   const int seq = (int)ci.seq, head = (int)ci.head, row_tile = (int)ci.part / T.split, stretch = (int)ci.part - row_tile * T.split;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
-  const Seq S = sequence(T, seq);
+  const Seq S = sequence(T, seq, tid == 0);
   const int rows = S.n * T.group, row0 = row_tile * ROWS;
   if (row0 >= rows) return;
   const int row1 = row0 + ROWS < rows ? row0 + ROWS : rows;
@@ -544,7 +584,7 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
   Attend<DT, D, R, false> a;
   a.clear();
   a.load_rows(T, S, head, row0, lane);
-  a.template run<W>(T, seq, head, S.length, begin + wave, end, see.hi, see.all_lo, see.all_hi, lane);
+  a.template run<W>(T, seq, head, S.length, begin + wave, end, see.lo, see.hi, see.all_lo, see.all_hi, lane);
 
   // all wavefronts' sums to one reference
   static_for<R>([&](auto J) {
@@ -717,15 +757,18 @@ __global__ __launch_bounds__(256) void st_attn_move_kernel(const AttnDev* table,
   constexpr int LPT = D / 8, TH = attn_move_count(D), kBlock = attn_block_bytes(D);
   const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
   ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
-  const int seq = (int)ci.seq, tid = (int)threadIdx.x, lane = tid & 63, c = tid % LPT, slot = tid / LPT;
-  const Seq S = sequence(T, seq);
+  const int tid = (int)threadIdx.x, lane = tid & 63, c = tid % LPT, slot = tid / LPT, kv = T.kv_heads, shift = T.page_shift;
+  int seq = (int)ci.seq, part = (int)ci.part;
+  if constexpr (TURNS > 1) {
+    if (!find_sequence(T, ci.seq, seq, part, [kv](int n) { return (int)(((int64_t)(n + 15) / 16 * 16 * kv + TURNS * TH - 1) / (TURNS * TH)); })) return;
+  }
+  const Seq S = sequence(T, seq, tid == 0);
   const int32_t* row_of_table = T.table + (int64_t)seq * T.table_pages;
-  const int kv = T.kv_heads, shift = T.page_shift;
   int j[TURNS], head[TURNS], page[TURNS];
   u32x4 k[TURNS], v[TURNS];
   static_for<TURNS>([&](auto N) {
     constexpr int n = decltype(N)::value;
-    const int th = ((int)ci.part * TURNS + n) * TH + slot;
+    const int th = (part * TURNS + n) * TH + slot;
     if constexpr (TURNS > 1) {            // 16 tokens of a head, then those of the next: a wavefront has tokens of one head
       const int group = __builtin_amdgcn_readfirstlane(th / 16);
       head[n] = group % kv;

@@ -24,6 +24,9 @@ struct OnDevice {
   OnDevice& operator=(const OnDevice&) = delete;
 };
 
+// A launch holds fewer than 2^32 threads, which its largest workgroups of 512 reach with this many.
+constexpr int64_t kMostWorkgroups = (int64_t)1 << 23;
+
 // What a matrix of rows spans; whether two of them share a byte.
 struct Span {
   uintptr_t at;

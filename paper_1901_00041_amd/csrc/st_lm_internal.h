@@ -90,6 +90,8 @@ struct AttnDev {
 static_assert(sizeof(AttnDev) == 208, "a multiple of 16 bytes for launch_poke");
 
 struct AttnItem { uint32_t tenant, seq, head, part; };   // part: row tile * split + stretch, or the stretch of new tokens
+// In place of a sequence: the part-th of all sequences' parts together, or a look at all their numbers (see find_sequence in st_attn.hip).
+constexpr uint32_t kAttnCheck = 0xffffffffu, kAttnFind = 0xfffffffeu;
 
 int launch_attn(int dtype, int dim, int kind, const AttnDev* table_dev, const AttnItem* items_dev, int64_t n_items, void* stream);
 // New tokens into the cache, or (read) out of it; part: the stretch of attn_move_count() of a sequence's new tokens x key heads, or (many: for

@@ -268,7 +268,7 @@ st_status build(st_matmul* p, const st_matmul_desc* descs, int n, const st_plan_
     p->totals.flops += 2 * (int64_t)d.M * d.N * d.K;
     p->totals.bytes += ((int64_t)d.M * d.K + (int64_t)d.N * d.K + ((d.epilogue & ST_EPI_BIAS) ? d.N : 0)) * es + (int64_t)d.M * d.N * os * ((d.epilogue & kResiduals) ? 2 : 1);
   }
-  if (p->totals.n_items >= ((int64_t)1 << 31)) return fail(ST_ERR_UNSUPPORTED, "more than 2^31 work items");
+  if (p->totals.n_items >= kMostWorkgroups) return fail(ST_ERR_UNSUPPORTED, "more than 2^23 workgroups");
   for (int dtype = 0; dtype < 3; ++dtype)
     for (int shape = 0; shape < kNumMatmulShapes; ++shape) {
       std::vector<int> mine;

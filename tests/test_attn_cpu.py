@@ -112,3 +112,20 @@ def test_oracle_elements():
     k[2, 5], k[3, 40] = np.inf, np.nan
     kc, ks, vc, vs = ah.encode_token_head(k, x)
     assert (ks[2:4] == 255).all() and (vs[2:4] == 1).all() and not kc[2:4].any() and not vc[2:4].any() and (ks[4:] < 255).all()
+
+
+def test_workgroups_follow_the_rows_that_there_can_be():
+    """max_new = max_tokens: the sequences together have no more rows than that."""
+    many = dict(n_seqs=1000, max_new=8192, max_tokens=8192, table_pages=256)
+    # 192 rows of a key head's four query heads to a workgroup, one more for what a sequence leaves of one, and one that looks at the numbers
+    assert st_lm.st_attn_get_info(plan(many)).n_items == 2 * (8192 * 4 // 192 + 1000) + 1
+    assert st_lm.st_attn_get_info(plan(dict(many, n_seqs=1))).n_items == 2 * -(-8192 * 4 // 192)
+
+
+def test_more_is_refused():
+    far = 1 << 40
+    for change, status in ((dict(k=0x70000000), sc.ST_ERR_INVALID_ARG), (dict(v=0x70000000 + 64), sc.ST_ERR_INVALID_ARG),
+                           (dict(n_seqs=1 << 20, max_new=1, kv_heads=8, out=far), sc.ST_ERR_UNSUPPORTED)):
+        with pytest.raises(sc.StError) as refused:
+            plan(change)
+        assert refused.value.status == status

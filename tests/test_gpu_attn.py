@@ -384,3 +384,88 @@ def test_far_pages(new):
     t.table[:, :4] -= far
     t.check_out()
     assert st_lm.st_attn_status(plan) == 0
+
+
+# ---- max_new far above what most sequences bring: the sequences of a launch's parts are looked up on the device ------------------------------
+
+LOOSE = [(n % 5 if n % 7 else 40 + n, 200 + 3 * n) for n in range(70)] + [(0, 9)] * 61 + [(300, 300), (1, 1), (0, 0)]
+
+
+def loose(seqs, dim=64, dtype="bf16", window=0, causal=True, max_new=4096):
+    t = Tenant(4, 2, dim, dtype, seqs, page=16, filled=False, max_new=max_new, window=window, causal=causal)
+    t.fill([length - n for n, length in t.seqs])
+    return t
+
+
+@pytest.mark.parametrize("dim, dtype, causal, window", [(64, "bf16", True, 0), (128, "f16", False, 0), (256, "bf16", True, 37)])
+def test_many_sequences_of_few_tokens_under_a_large_max_new(dim, dtype, causal, window):
+    torch = torch_()
+    t = loose(LOOSE, dim, dtype, window, causal)
+    listed = loose(LOOSE, dim, dtype, window, causal, max_new=300)
+    plan = make_plan([t])
+    # not more workgroups than all rows can make, which a bound for each sequence by itself would exceed by far
+    assert st_lm.st_attn_get_info(plan).n_items < 2 * (t.tokens + len(LOOSE)) + 2 < 2 * len(LOOSE) * (4096 * 2 // 256)
+    other = make_plan([listed])
+    for p in (plan, other):
+        st_lm.st_attn_append(p)
+        st_lm.st_attn_read(p)
+        st_lm.st_attn_run(p)
+    torch.cuda.synchronize()
+    t.fill([length for _, length in t.seqs])
+    t.check_out()
+    assert np.array_equal(t.d["pages"].cpu().numpy(), t.pool.bytes)
+    for name in ("out", "k_out", "v_out"):
+        t.check_untouched("", name)
+        assert torch.equal(t.d[name].view(torch.int16), listed.d[name].view(torch.int16)), name
+    assert st_lm.st_attn_status(plan) == 0
+
+
+def test_numbers_outside_the_descriptor_under_a_large_max_new():
+    torch = torch_()
+    for change, which, calls in ((dict(length=-5), 3, "run"), (dict(length=-5), 80, "append"), (dict(first=1 << 30), 100, "run"), (dict(first=-1), 131, "append"), (dict(length=1 << 30), 75, "read")):
+        t = loose(LOOSE)
+        for name, value in change.items():
+            getattr(t, name)[which] = value
+        if "length" in change and which == 3:
+            assert t.seqs[3][0] > 0
+        t.table[:, -1] = t.table[0, 0]
+        t.table[t.table == 1 << 30] = t.table[0, 0]
+        plan = make_plan([t])
+        torch.cuda.synchronize()
+        getattr(st_lm, "st_attn_" + calls)(plan)
+        assert st_lm.st_attn_status(plan) == st_lm.ST_ATTN_BAD_LENGTH, (change, which)
+        assert st_lm.st_attn_status(plan) == 0
+
+
+@pytest.mark.parametrize("dim", [64, 256])
+@pytest.mark.parametrize("new", [1, 20, 100])
+def test_pages_before_the_window_may_be_gone(new, dim):
+    """Their entries may hold anything, and nothing is reported."""
+    torch = torch_()
+    t = Tenant(4, 2, dim, "bf16", [(new, 300), (new, 161), (new, new)], page=16, window=33)
+    k = [t.held(s) for s in range(3)]
+    t.held = lambda s: k[s]
+    for s, (n, length) in enumerate(t.seqs):
+        gone = max(0, length - n - 33 + 1) // 16
+        t.table[s, :gone] = -1
+    plan = run(t)
+    t.check_out()
+    assert st_lm.st_attn_status(plan) == 0
+
+
+def test_no_pages_are_reported():
+    torch = torch_()
+    t = Tenant(2, 1, 64, "bf16", [(1, 5)], page=16)
+    for new in (1, 64):
+        plan = st_lm.st_attn_plan([t.upload().desc(n_pages=0, pages=None, max_new=new)], keep=t)
+        st_lm.st_attn_run(plan)
+        torch.cuda.synchronize()
+        assert not t.outputs()[:1].any() and st_lm.st_attn_status(plan) == st_lm.ST_ATTN_BAD_PAGE
+
+
+def test_the_largest_scale():
+    """All scores of one value: the softmax is even, whatever the scale."""
+    torch = torch_()
+    t = Tenant(2, 1, 64, "bf16", [(1, 50), (40, 60)], page=16, scale=3.0e38, gain=0.0)
+    run(t)
+    t.check_out()
