@@ -94,7 +94,6 @@ int most_steps(const st_attn_desc& d) {      // that a row tile of single tokens
   if (d.window) tokens = std::min(tokens, (int64_t)d.window + d.max_new + kAttnStep);
   return cdiv(tokens, kAttnStep) + 1;
 }
-constexpr int kAttnMostSteps = 192, kAttnWholeSteps = 40;
 // Few rows: the tokens are divided among wavefronts and workgroups; else the rows are.
 int kind_of(const st_attn_desc& d) {
   const int rows = most_rows(d);
@@ -121,6 +120,22 @@ int64_t all_row_tiles(const st_attn_desc& d) {
 }
 bool find_rows(const st_attn_desc& d, int64_t row_tiles) { return kind_of(d) == kAttnRows && d.n_seqs * row_tiles > kAttnLoose * all_row_tiles(d); }
 
+// Rows whose tokens are divided.  A stretch's tile of tokens takes some 1.7 us, and 2.9 where two workgroups share a compute unit (one does
+// with heads of 256: 1.3); the last workgroup reads each stretch's sums in 2.8 us (5.5): sqrt(root tiles) stretches take least time, as
+// far as there is room for them.  Either one workgroup to a compute unit, or two, if that makes nearly twice as many stretches.  Between one and
+// two the chip is filled unevenly, and many short stretches even that out.  In us, whole and divided (heads 32 and 8 of 128): 512 new tokens of
+// 16384 430 and 159 (in 5), of 4096 112 and 58 (5), 128 of 8192 215 and 50 (9), 64 of 32768 843 and 89 (16), 2048 of 8192 304 and 254 (5).
+constexpr int kMostRowSplit = 16;
+void row_stretches(AttnDev& T, const st_attn_desc& d, double tiles, int most_steps) {
+  const int one = std::max(1, (int)(kNumCUs / tiles)), two = d.head_dim == 256 ? one : std::max(1, (int)(2 * kNumCUs / tiles));
+  T.root = d.head_dim == 256 ? 0.24f : 0.62f;
+  T.whole = d.head_dim == 256 ? 20 : 8;
+  T.want = std::min(one, kMostRowSplit);
+  T.most = std::min(two > 1.8 * one ? two : one, kMostRowSplit);
+  if (tiles > kNumCUs && tiles < 1.6 * kNumCUs && d.head_dim != 256) T.want = 3, T.most = 5;
+  T.split = most_steps <= T.whole ? 1 : std::max(1, std::min(T.most, (int)(std::sqrt((double)most_steps * T.root) + 1.0)));
+}
+
 st_status upload(st_attn* p) {
   const size_t n = p->tenants.size();
   auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
@@ -128,10 +143,11 @@ st_status upload(st_attn* p) {
   size_t all_tiles = 0, all_floats = 0;
   for (size_t t = 0; t < n; ++t) {
     const AttnDev& T = p->tenants[t];
-    const int kind = kind_of(p->descs[t]);
-    if (kind == kAttnRows || T.split <= 1) continue;
-    tiles[t] = (size_t)T.n_seqs * T.kv_heads * T.row_tiles;
-    floats[t] = tiles[t] * T.split * (size_t)(16 * attn_blocks(kind, p->descs[t].head_dim)) * (size_t)(p->descs[t].head_dim + 2);
+    const st_attn_desc& d = p->descs[t];
+    const int kind = kind_of(d);
+    if (T.split <= 1) continue;
+    tiles[t] = (size_t)T.kv_heads * (size_t)(find_rows(d, T.row_tiles) ? all_row_tiles(d) : (int64_t)T.n_seqs * T.row_tiles);
+    floats[t] = tiles[t] * T.split * (size_t)(kind == kAttnRows ? attn_row_slot(kind, d.head_dim) : 16 * attn_blocks(kind, d.head_dim) * (d.head_dim + 2));
     all_tiles += tiles[t];
     all_floats += floats[t];
   }
@@ -165,7 +181,7 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
   p->tenants.assign((size_t)n, AttnDev{});
   p->totals.n_tenants = n;
   p->totals.host_only = o.host_only;
-  double tiles = 0;      // of tenants whose tokens are divided, all together
+  double tiles = 0, row_tiles = 0;      // of all tenants of either kind
   for (int t = 0; t < n; ++t) {
     const st_attn_desc& d = descs[t];
     const int kind = kind_of(d);
@@ -184,31 +200,33 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
     T.flip = d.scale < 0 ? 0x80008000u : 0u;
     T.row_tiles = cdiv(most_rows(d), (kind == kAttnRows ? attn_row_waves(d.head_dim) : 1) * 16 * attn_blocks(kind, d.head_dim));
     T.split = 1;
-    T.chunk = 1 << 30;
-    if (d.max_tokens > 0 && kind != kAttnRows) tiles += (double)d.n_seqs * d.kv_heads * T.row_tiles;
+    if (d.max_tokens > 0 && d.n_seqs > 0 && kind != kAttnRows) tiles += (double)d.n_seqs * d.kv_heads * T.row_tiles;
+    if (d.max_tokens > 0 && d.n_seqs > 0 && kind == kAttnRows) row_tiles += (double)std::min((int64_t)d.n_seqs * T.row_tiles, all_row_tiles(d)) * d.kv_heads;
   }
   int64_t n_items = 0, n_moves = 0;
   for (int t = 0; t < n; ++t) {
     const st_attn_desc& d = descs[t];
     AttnDev& T = p->tenants[t];
     if (d.n_seqs == 0 || d.max_tokens == 0) continue;
+    const int steps = most_steps(d);
     if (kind_of(d) != kAttnRows) {
-      const int steps = most_steps(d);
-      int chunk;
-      if (o.split_k > 0) {
-        chunk = cdiv(steps, std::min(o.split_k, kAttnMaxSplit));
-      } else {
-        // A stretch on every compute unit: more of them only cost their set-up and their joining (one context of 131072, us with 24, 32, 64
-        // stretches: 35.3, 36.9, 42.9; 32 of 8000 with heads of 256, 128, 256, 512 workgroups: 43.1, 28.4, 36.3).  But none longer
-        // than 192 steps, or a few long sequences outlast the others (64 of up to 8192: 75.5 us in one stretch each, 66.9 in two),
-        // and short ones whole (a single sequence of 1000: 8.2 us whole, 9.1 in two; of 2000: 12.0 whole, 9.5 in four; of 4000: 19.9, 9.9 in eight).
-        const int want = std::max(1, std::min(kAttnMaxSplit, (int)std::ceil(kNumCUs / tiles)));
-        chunk = steps <= kAttnWholeSteps ? steps : std::max(2 * kAttnTokenWaves, cdiv(steps, std::max(want, std::min(kAttnMaxSplit, cdiv(steps, kAttnMostSteps)))));
-      }
-      T.chunk = chunk;
-      T.split = cdiv(steps, chunk);
+      // A stretch on every compute unit: more of them only cost their set-up and their joining (one context of 131072, us with 24, 32, 64
+      // stretches: 35.3, 36.9, 42.9; 32 of 8000 with heads of 256, 128, 256, 512 workgroups: 43.1, 28.4, 36.3).  But none longer
+      // than 192 steps, or a few long sequences outlast the others (64 of up to 8192: 75.5 us in one stretch each, 66.9 in two),
+      // and short ones whole (a single sequence of 1000: 8.2 us whole, 9.1 in two; of 2000: 12.0 whole, 9.5 in four; of 4000: 19.9, 9.9 in eight).
+      T.want = std::max(1, std::min(kAttnMaxSplit, (int)std::ceil(kNumCUs / tiles)));
+      T.whole = 40; T.most = 192; T.least = 2 * kAttnTokenWaves;
+      if (o.split_k > 0) T.want = std::min(o.split_k, kAttnMaxSplit), T.whole = 0, T.most = 1 << 30, T.least = 1;
+      // ... as far as the table has no more room than is used: 2048 workgroups in all, as those of stretches that there are not take time, too
+      const int parts = std::max(T.want, std::min({kAttnMaxSplit, cdiv(steps, T.most), (int)std::max(1.0, 2048 / tiles)}));
+      T.split = steps <= T.whole ? 1 : std::min(parts, cdiv(steps, T.least));
+      T.want = std::min(T.want, T.split);
+      T.chunk = std::max(T.least, cdiv(steps, T.split));
+    } else {
+      row_stretches(T, d, row_tiles, steps / (attn_row_tokens(d.head_dim) / kAttnStep) + 2);
+      if (o.split_k > 0) T.split = T.want = T.most = std::min(o.split_k, kMostRowSplit), T.root = 1e12f, T.whole = 0;
     }
-    n_items += find_rows(d, T.row_tiles) ? all_row_tiles(d) * d.kv_heads + 1 : (int64_t)d.n_seqs * d.kv_heads * T.row_tiles * T.split;
+    n_items += find_rows(d, T.row_tiles) ? all_row_tiles(d) * d.kv_heads * T.split + 1 : (int64_t)d.n_seqs * d.kv_heads * T.row_tiles * T.split;
     n_moves += find_moves(d) ? all_moves(d) + 1 : d.n_seqs * move_parts(d);
     if (n_items >= kMostWorkgroups || n_moves >= kMostWorkgroups) return fail(ST_ERR_UNSUPPORTED, "more than 2^23 workgroups");
   }
@@ -219,19 +237,19 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
         for (int t = 0; t < n; ++t) {
           const st_attn_desc& d = descs[t];
           const AttnDev& T = p->tenants[t];
-          if (d.dtype != dtype || d.head_dim != dim || kind_of(d) != kind || d.n_seqs == 0 || d.max_tokens == 0) continue;
+          if (d.dtype != dtype || d.head_dim != dim || (kind_of(d) == kAttnRows && T.split > 1 ? kAttnRowsSplit : kind_of(d)) != kind || d.n_seqs == 0 || d.max_tokens == 0) continue;
           if (find_rows(d, T.row_tiles)) {
             p->items.push_back({(uint32_t)t, kAttnCheck, 0u, 0u});
-            for (int64_t part = 0; part < all_row_tiles(d); ++part)
-              for (int h = 0; h < d.kv_heads; ++h) p->items.push_back({(uint32_t)t, kAttnFind, (uint32_t)h, (uint32_t)part});
+            for (int stretch = 0; stretch < T.split; ++stretch)
+              for (int64_t tile = 0; tile < all_row_tiles(d); ++tile)
+                for (int h = 0; h < d.kv_heads; ++h) p->items.push_back({(uint32_t)t, kAttnFind, (uint32_t)h, (uint32_t)(tile * T.split + stretch)});
             continue;
           }
           // a sequence's last rows see most; a key head's row tiles stay on one XCD where the heads divide well
-          const int parts = T.row_tiles * T.split;
-          for (int part = 0; part < parts; ++part)
-            for (int s = 0; s < d.n_seqs; ++s)
-              for (int h = 0; h < d.kv_heads; ++h)
-                p->items.push_back({(uint32_t)t, (uint32_t)s, (uint32_t)h, (uint32_t)(kind == kAttnRows ? parts - 1 - part : part)});
+          for (int stretch = 0; stretch < T.split; ++stretch)      // stretches that there are not, come last
+            for (int tile = T.row_tiles - 1; tile >= 0; --tile)
+              for (int s = 0; s < d.n_seqs; ++s)
+                for (int h = 0; h < d.kv_heads; ++h) p->items.push_back({(uint32_t)t, (uint32_t)s, (uint32_t)h, (uint32_t)(tile * T.split + stretch)});
         }
         if ((int64_t)p->items.size() > begin) p->runs.push_back({dtype, dim, kind, begin, (int64_t)p->items.size() - begin});
       }

@@ -356,6 +356,20 @@ struct Attend {
   }
 };
 
+// A stretch's steps, of so many.  The division goes by what there is, not by what the table has room for.
+__device__ __forceinline__ int tokens_chunk(int steps, ConstAttn& T) {
+  if (steps <= T.whole) return steps > 0 ? steps : 1;
+  const int by_length = (steps + T.most - 1) / T.most, parts = by_length < T.split ? by_length : T.split, want = parts > T.want ? parts : T.want;
+  int chunk = (steps + want - 1) / want;
+  chunk = chunk > T.least ? chunk : T.least;
+  return chunk < T.chunk ? chunk : T.chunk;
+}
+__device__ __forceinline__ int rows_chunk(int steps, ConstAttn& T) {
+  if (steps <= T.whole) return steps;
+  const int best = (int)(__builtin_amdgcn_sqrtf((float)steps * T.root) + 0.5f), few = best < T.want ? best : T.want, parts = best >= T.most ? T.most : few;
+  return parts > 1 ? (steps + parts - 1) / parts : steps;
+}
+
 // The tokens that rows [row0, row1) of a sequence see: any of them, and all of them.
 struct Seen { int lo, hi, all_lo, all_hi; };
 __device__ __forceinline__ Seen seen_by(ConstAttn& T, const Seq& S, int row0, int row1) {
@@ -385,10 +399,13 @@ __device__ __forceinline__ void store_out(ConstAttn& T, const Seq& S, int head, 
 // one) into LDS, in operand order (fragment f, lane l at 16 bytes (64 f + l)), while all compute on the present one: two buffers, one
 // barrier a tile.  A wavefront issues a vector instruction every five to six clocks at best and its MFMAs take sixteen each, so the
 // widening is cut into pieces that are issued between MFMAs.
-template <int DT, int D, int R>
+//
+// SPLIT: few rows over many tokens, which are divided into stretches.  A stretch's sums lie in memory as they lie in the lanes, and whoever
+// arrives last adds them up in order.
+template <int DT, int D, int R, bool SPLIT>
 __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel(const AttnDev* table, const AttnItem* items) {
   typedef Attend<DT, D, R, true> A;
-  constexpr int W = attn_row_waves(D), TT = D == 256 ? 32 : 64, BLOCKS = TT / 16, KW = A::KW, NE = A::NE;
+  constexpr int W = attn_row_waves(D), TT = attn_row_tokens(D), BLOCKS = TT / 16, KW = A::KW, NE = A::NE;
   constexpr int SHARE = W / BLOCKS;                                     // wavefronts to a block
   constexpr int KWAVE = KW / SHARE, VWAVE = NE / SHARE;                 // fragments that a wavefront makes of its block's keys and values
   constexpr int KF = BLOCKS * KW, VF = TT / 32 * NE;                    // fragments of a tile
@@ -398,8 +415,8 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
   const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
   ConstAttn& T = ((ConstAttn*)table)[ci.tenant];
   constexpr int ROWS = W * 16 * R;
-  int seq, part_of = (int)ci.part;
-  const int group = T.group;
+  const int group = T.group, split = SPLIT ? T.split : 1, item = SPLIT ? (int)ci.part / split : (int)ci.part, stretch = SPLIT ? (int)ci.part - item * split : 0;
+  int seq, part_of = item;
   if (!find_sequence(T, ci.seq, seq, part_of, [group](int n) { return (n * group + ROWS - 1) / ROWS; })) return;
   const int head = (int)ci.head;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
@@ -411,10 +428,20 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
   const Seen all = seen_by(T, S, block0, block1);
   Seen see = seen_by(T, S, row0 < rows ? row0 : block0, row0 < rows ? row1 : block1);
   if (row0 >= rows) see.hi = -1;                                         // helps widening, has nothing to compute
+  int n0 = all.lo / TT, n1 = all.hi >= all.lo ? all.hi / TT + 1 : n0, active = 1;
+  if constexpr (SPLIT) {      // stretches as long as those of the sequence's last rows, so that all take about as long
+    const int most = T.window && T.window + ROWS < S.length ? T.window + ROWS : S.length;
+    const int chunk = rows_chunk((most + TT - 1) / TT + 1, T);
+    active = n1 - n0 > chunk ? (n1 - n0 + chunk - 1) / chunk : 1;
+    if (stretch >= active) return;
+    if (active > 1) {
+      n0 += stretch * chunk;
+      n1 = stretch + 1 < active ? n0 + chunk : n1;
+    }
+  }
   A a;
   a.clear();
   a.load_rows(T, S, head, row0, lane);
-  const int n0 = all.lo / TT, n1 = all.hi >= all.lo ? all.hi / TT + 1 : n0;
   const int kb = wave / SHARE, part = wave % SHARE;                     // the wavefront's block of a tile, and its part of it
 
   struct Raw { uint32_t k[KWAVE], v[4], ks, vs; int page; };            // the part as it lies in the cache; v: a word per token (D = 64: per two)
@@ -540,6 +567,56 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
     }
   }
   if (bad_pages && lane == 0) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_PAGE);
+  if constexpr (SPLIT) {
+    if (active > 1) {
+      __shared__ uint32_t flag;
+      constexpr int THREADS = W * 64, kVectors = NE * R, kSlot = attn_row_slot(kAttnRows, D) * 4;
+      const int tid = (int)threadIdx.x;
+      const int64_t tile = ci.seq == kAttnFind ? (int64_t)item * T.kv_heads + head : ((int64_t)seq * T.kv_heads + head) * T.row_tiles + item;
+      float* slots = T.ws + tile * split * (kSlot / 4);
+      const __amdgpu_buffer_rsrc_t rs = make_rsrc(slots + (int64_t)stretch * (kSlot / 4), kSlot);
+      static_for<kVectors>([&](auto Q) {
+        constexpr int q = decltype(Q)::value;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, a.acc[q / R][q % R]), rs, tid * 16 + q * THREADS * 16, 0, kAuxDeviceCoherent);
+      });
+      static_for<R>([&](auto J) {
+        constexpr int r = decltype(J)::value;
+        const u32x2 stat = {__builtin_bit_cast(uint32_t, a.m[r]), __builtin_bit_cast(uint32_t, a.sum[r][0])};
+        __builtin_amdgcn_raw_buffer_store_b64(stat, rs, tid * 8 + kVectors * THREADS * 16 + r * THREADS * 8, 0, kAuxDeviceCoherent);
+      });
+      __builtin_amdgcn_s_waitcnt(0);      // this thread's stores have been written through
+      __builtin_amdgcn_sched_barrier(0);
+      __syncthreads();
+      if (tid == 0) {
+        const uint32_t old = __hip_atomic_fetch_add(&T.counters[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t is_last = old == (uint32_t)(active - 1);
+        if (is_last) __hip_atomic_store(&T.counters[tile], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        flag = is_last;
+      }
+      __syncthreads();
+      if (flag == 0u) return;
+      auto stat_of = [&](int s, int r) __attribute__((always_inline)) {
+        return __builtin_amdgcn_raw_buffer_load_b64(make_rsrc(slots + (int64_t)s * (kSlot / 4), kSlot), tid * 8 + kVectors * THREADS * 16 + r * THREADS * 8, 0, kAuxDeviceCoherent);
+      };
+      a.clear();
+      for (int s = 0; s < active; ++s)
+        static_for<R>([&](auto J) { a.m[decltype(J)::value] = fmaxf(a.m[decltype(J)::value], __builtin_bit_cast(float, stat_of(s, decltype(J)::value)[0])); });
+      for (int s = 0; s < active; ++s) {
+        const __amdgpu_buffer_rsrc_t from = make_rsrc(slots + (int64_t)s * (kSlot / 4), kSlot);
+        float w[R];
+        static_for<R>([&](auto J) {
+          constexpr int r = decltype(J)::value;
+          const u32x2 stat = stat_of(s, r);
+          w[r] = __builtin_amdgcn_exp2f(__builtin_bit_cast(float, (uint32_t)stat[0]) - a.m[r]);
+          a.sum[r][0] += w[r] * __builtin_bit_cast(float, (uint32_t)stat[1]);
+        });
+        static_for<kVectors>([&](auto Q) {
+          constexpr int q = decltype(Q)::value;
+          a.acc[q / R][q % R] += w[q % R] * __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, tid * 16 + q * THREADS * 16, 0, kAuxDeviceCoherent));
+        });
+      }
+    }
+  }
   static_for<R>([&](auto J) {
     constexpr int r = decltype(J)::value;
     const int row = row0 + r * 16 + i;
@@ -577,9 +654,9 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
   const int row1 = row0 + ROWS < rows ? row0 + ROWS : rows;
   const Seen see = seen_by(T, S, row0, row1);
   const int s_lo = see.lo / kAttnStep, steps = see.hi >= see.lo ? see.hi / kAttnStep + 1 - s_lo : 0;
-  const int active = steps > T.chunk ? (steps + T.chunk - 1) / T.chunk : 1;      // stretches that there are
+  const int chunk = tokens_chunk(steps, T), active = steps > chunk ? (steps + chunk - 1) / chunk : 1;      // stretches that there are
   if (stretch >= active) return;
-  const int begin = s_lo + stretch * T.chunk, end = stretch + 1 < active ? begin + T.chunk : s_lo + steps;
+  const int begin = s_lo + stretch * chunk, end = stretch + 1 < active ? begin + chunk : s_lo + steps;
 
   Attend<DT, D, R, false> a;
   a.clear();
@@ -841,7 +918,8 @@ static hipError_t launch_kind(int kind, unsigned blocks, void* stream, const Att
   switch (kind) {
     case kAttnTokens1: return launch(st_attn_tokens_kernel<DT, D, attn_blocks(kAttnTokens1, D)>, blocks, kAttnTokenWaves * 64, stream, table, items);
     case kAttnTokens2: return launch(st_attn_tokens_kernel<DT, D, attn_blocks(kAttnTokens2, D)>, blocks, kAttnTokenWaves * 64, stream, table, items);
-    case kAttnRows: return launch(st_attn_rows_kernel<DT, D, attn_blocks(kAttnRows, D)>, blocks, attn_row_waves(D) * 64, stream, table, items);
+    case kAttnRows: return launch(st_attn_rows_kernel<DT, D, attn_blocks(kAttnRows, D), false>, blocks, attn_row_waves(D) * 64, stream, table, items);
+    case kAttnRowsSplit: return launch(st_attn_rows_kernel<DT, D, attn_blocks(kAttnRows, D), true>, blocks, attn_row_waves(D) * 64, stream, table, items);
   }
   return hipErrorInvalidValue;
 }

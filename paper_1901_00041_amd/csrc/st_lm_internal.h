@@ -55,10 +55,14 @@ constexpr int kAttnBlock = 16;           // tokens per cache block
 constexpr int kAttnStep = 32;            // tokens per step of a wavefront
 constexpr int kAttnTokenWaves = 8;
 constexpr int attn_row_waves(int dim) { return dim == 256 ? 8 : 4; }
+constexpr int attn_row_tokens(int dim) { return dim == 256 ? 32 : 64; }      // of a tile that they widen together
 constexpr int kAttnMaxSplit = 64;
-constexpr int kAttnTokens1 = 0, kAttnTokens2 = 1, kAttnRows = 2, kNumAttnKinds = 3;
+constexpr int kAttnTokens1 = 0, kAttnTokens2 = 1, kAttnRows = 2, kAttnRowsSplit = 3, kNumAttnKinds = 4;      // RowsSplit: its tokens are divided, too
 // R of a kind: rows are as many as the registers hold beside their queries, scores and outputs
 constexpr int attn_blocks(int kind, int dim) { return kind == kAttnTokens1 ? 1 : kind == kAttnTokens2 ? (dim == 256 ? 1 : 2) : dim == 64 ? 4 : dim == 128 ? 3 : 1; }
+
+// Floats of a stretch's partial result with kAttnRowsSplit: each thread's outputs, maxima and sums.
+constexpr int attn_row_slot(int kind, int dim) { return attn_row_waves(dim) * 64 * attn_blocks(kind, dim) * (dim / 4 + 2); }
 
 // Bytes of a block of 16 tokens of one head, and where its parts begin.
 constexpr int attn_block_bytes(int dim) { return kAttnBlock * (dim + dim / 16); }
@@ -74,7 +78,7 @@ struct AttnDev {
   const int32_t* table;
   const int32_t* first;
   const int32_t* length;
-  float* ws;             // partial results: [tile][split][rows][dim], then their maxima and sums, [tile][split][2][rows]
+  float* ws;             // partial results: [tile][split][rows][dim], then their maxima and sums, [tile][split][2][rows]; with kAttnRowsSplit slots
   uint32_t* counters;    // one arrival counter per tile, zero between runs
   uint32_t* status;      // ST_ATTN_BAD_* that runs have met
   int64_t ldq, ldk, ldv, ldo;
@@ -84,10 +88,18 @@ struct AttnDev {
   int32_t table_pages, window, causal;
   float scale;           // its size times log2(e), above zero
   int32_t row_tiles;     // per sequence and key head
-  int32_t split, chunk;  // at most `split` stretches of `chunk` steps
+  int32_t split;         // at most so many stretches.  How many, of wavefronts that take turns:
+  int32_t whole;         // one for no more steps than these, else
+  int32_t want;          // these, or
+  int32_t most;          // so many that none has more steps than these, but
+  int32_t least;         // so few that none but the last has fewer than these, and
+  int32_t chunk;         // none has more than these.
+  float root;            // With kAttnRowsSplit (a step: a tile of the workgroup): one up to `whole` steps, else the square root of root times the
+                         // steps, if that is `most` or more just these, else not more than `want`
   uint32_t flip;         // sign bits of two query elements, where scale is negative
+  int32_t pad[3];
 };
-static_assert(sizeof(AttnDev) == 208, "a multiple of 16 bytes for launch_poke");
+static_assert(sizeof(AttnDev) == 240, "a multiple of 16 bytes for launch_poke");
 
 struct AttnItem { uint32_t tenant, seq, head, part; };   // part: row tile * split + stretch, or the stretch of new tokens
 // In place of a sequence: the part-th of all sequences' parts together, or a look at all their numbers (see find_sequence in st_attn.hip).

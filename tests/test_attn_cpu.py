@@ -78,7 +78,9 @@ def test_plans_divide_long_lengths():
     assert st_lm.st_attn_get_info(plan(long)).n_items > 2 and st_lm.st_attn_get_info(plan(long)).workspace_bytes > 0
     assert st_lm.st_attn_get_info(plan(dict(long, window=100))).n_items == 2          # a window is short
     assert st_lm.st_attn_get_info(plan(long, split_k=1)).workspace_bytes == 0
-    assert st_lm.st_attn_get_info(plan(dict(long, max_new=500))).workspace_bytes == 0  # many rows
+    many = dict(long, max_new=500, max_tokens=500)
+    assert st_lm.st_attn_get_info(plan(many)).workspace_bytes > 0                      # many rows, but few beside the chip
+    assert st_lm.st_attn_get_info(plan(dict(many, n_seqs=100, max_tokens=50000))).workspace_bytes == 0
     both = st_lm.st_attn_get_info(plan(long, dict(long, dtype="f16"), dict(long, head_dim=64, ldq=0)))
     assert both.launches == 3
 
@@ -119,7 +121,7 @@ def test_workgroups_follow_the_rows_that_there_can_be():
     many = dict(n_seqs=1000, max_new=8192, max_tokens=8192, table_pages=256)
     # 192 rows of a key head's four query heads to a workgroup, one more for what a sequence leaves of one, and one that looks at the numbers
     assert st_lm.st_attn_get_info(plan(many)).n_items == 2 * (8192 * 4 // 192 + 1000) + 1
-    assert st_lm.st_attn_get_info(plan(dict(many, n_seqs=1))).n_items == 2 * -(-8192 * 4 // 192)
+    assert st_lm.st_attn_get_info(plan(dict(many, n_seqs=1), split_k=1)).n_items == 2 * -(-8192 * 4 // 192)
 
 
 def test_more_is_refused():

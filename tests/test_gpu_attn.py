@@ -469,3 +469,38 @@ def test_the_largest_scale():
     t = Tenant(2, 1, 64, "bf16", [(1, 50), (40, 60)], page=16, scale=3.0e38, gain=0.0)
     run(t)
     t.check_out()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("split, causal, window, max_new", [(0, True, 0, None), (2, True, 0, None), (3, False, 0, None), (16, True, 0, None), (5, True, 150, None), (4, True, 0, 4096)])
+def test_divided_lengths_of_many_rows(split, causal, window, max_new, dim, dtype):
+    """Rows whose tokens are divided among workgroups: the same result every time, rows of one token and of none among them."""
+    torch = torch_()
+    seqs = [(70, 1500), (0, 40), (1, 1), (40, 40), (1, 1100), (33, 700), (130, 130), (0, 0)]
+    t = Tenant(4, 2, dim, dtype, seqs, page=32, causal=causal, window=window, max_new=max_new)
+    t.table[:, -1] = 0                                # room for far more tokens than there are
+    plan = st_lm.st_attn_plan([t.upload().desc()], sc.plan_opts(split_k=split), keep=t)
+    assert st_lm.st_attn_get_info(plan).workspace_bytes > 0
+    torch.cuda.synchronize()
+    st_lm.st_attn_run(plan)
+    torch.cuda.synchronize()
+    t.check_out()
+    once = t.d["out"].clone()
+    for _ in range(3):
+        t.d["out"].fill_(float("nan"))
+        st_lm.st_attn_run(plan)
+    assert st_lm.st_attn_status(plan) == 0
+    assert torch.equal(once.view(torch.int16), t.d["out"].view(torch.int16))
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_a_table_with_far_more_room_than_tokens(new):
+    """A captured plan's table is as wide as its sequences may ever get."""
+    torch = torch_()
+    t = Tenant(8, 2, 128, "bf16", [(new, 2000), (new, new), (0, 5)], page=16)
+    t.table = np.concatenate([t.table, np.full((3, 5000), 1 << 30, np.int32)], 1)
+    t.columns += 5000
+    plan = run(t)
+    t.check_out()
+    assert st_lm.st_attn_status(plan) == 0
