@@ -359,9 +359,10 @@ struct Attend {
 // A stretch's steps, of so many.  The division goes by what there is, not by what the table has room for.
 __device__ __forceinline__ int tokens_chunk(int steps, ConstAttn& T) {
   if (steps <= T.whole) return steps > 0 ? steps : 1;
-  const int by_length = (steps + T.most - 1) / T.most, parts = by_length < T.split ? by_length : T.split, want = parts > T.want ? parts : T.want;
-  int chunk = (steps + want - 1) / want;
-  chunk = chunk > T.least ? chunk : T.least;
+  // where the sequences alone fill the chip, stretches of one length, not halves: the short ones left over fill the gaps (64 of up to 8192: 67.6 us, 68.3)
+  const int one = T.most < T.chunk ? T.most : T.chunk, want = T.want > 1 ? T.want : T.split, even = (steps + want - 1) / want;
+  if (T.want == 1) return even > one ? even : one;
+  const int chunk = even > T.least ? even : T.least;
   return chunk < T.chunk ? chunk : T.chunk;
 }
 __device__ __forceinline__ int rows_chunk(int steps, ConstAttn& T) {

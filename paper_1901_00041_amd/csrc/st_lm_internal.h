@@ -90,8 +90,8 @@ struct AttnDev {
   int32_t row_tiles;     // per sequence and key head
   int32_t split;         // at most so many stretches.  How many, of wavefronts that take turns:
   int32_t whole;         // one for no more steps than these, else
-  int32_t want;          // these, or
-  int32_t most;          // so many that none has more steps than these, but
+  int32_t want;          // these, or, if it is one, so many that
+  int32_t most;          // none has more steps than these, but
   int32_t least;         // so few that none but the last has fewer than these, and
   int32_t chunk;         // none has more than these.
   float root;            // With kAttnRowsSplit (a step: a tile of the workgroup): one up to `whole` steps, else the square root of root times the
