@@ -70,7 +70,7 @@ typedef struct st_matmul st_matmul; /* opaque */
 /* Validates the descriptors, picks a tile shape and a division of the reduction per tenant, lists the work items and uploads
  * them.  Of opts (NULL: defaults) tile_cfg, split_k and host_only are read, as in st_conv_plan.
  * n_tenants = 0, or M = 0 everywhere, gives a plan whose runs do nothing.
- * ST_ERR_UNSUPPORTED: a row longer than 2^20 elements or rows further apart than 2^21; more than 2^31 tiles. */
+ * ST_ERR_UNSUPPORTED: a row longer than 2^20 elements or rows further apart than 2^21; 2^23 workgroups or more. */
 st_status st_matmul_plan(const st_matmul_desc* descs, int32_t n_tenants, const st_plan_opts* opts, st_matmul** out_plan);
 st_status st_matmul_run(const st_matmul* plan, void* hip_stream);
 /* All tenants' pointers at once, in stream order (as st_conv_plan_rebind_all): x, w, bias, y and residual are taken from descs,
@@ -108,7 +108,9 @@ int32_t st_matmul_tile_count(void);
  *
  * What a run finds there is checked: a page index outside the pool is not followed (its tokens are not written, and hide from
  * every query); first is held to [0, max_tokens], what a sequence has more of than max_new new tokens are left out (the rows behind
- * them are left as they are), and a length is held to [0, table_pages * page_tokens].  st_attn_status reports that it happened. */
+ * them are left as they are), and a length is held to [0, table_pages * page_tokens].  st_attn_status reports that it happened, and that a
+ * sequence has more new tokens than tokens: those before its start see nothing (zeros), are not written and read as 0.  Attention does not
+ * report pages that no new token of the sequence sees (all of it before their windows): they may be gone, and their entries hold anything. */
 enum { ST_ATTN_CAUSAL = 1u };
 enum { ST_ATTN_BAD_PAGE = 1, ST_ATTN_BAD_LENGTH = 2 };
 
@@ -123,7 +125,7 @@ typedef struct st_attn_desc {
   int32_t n_pages, page_tokens, table_pages;   /* page_tokens 16, 32, 64, ..., 1024                                         */
   int32_t window;            /* > 0 (causal only): a token sees itself and the window - 1 tokens before it; 0: all           */
   uint32_t flags;            /* ST_ATTN_CAUSAL: token p sees tokens 0 .. p of its sequence; else all length[i] of them       */
-  float scale;               /* of the scores, before the softmax; finite                                                   */
+  float scale;               /* of the scores, before the softmax; finite; its size counts as 6e-31 at least, 2e38 at most   */
   int32_t reserved;          /* must be 0                                                                                   */
   int64_t ldq, ldk, ldv, ldo; /* elements from a row to the next of q, k (and k_out), v (and v_out), out; 0 = dense          */
   const void* q;             /* [max_tokens][heads][head_dim], for st_attn_run                                              */
@@ -148,9 +150,15 @@ typedef struct st_attn st_attn; /* opaque */
 
 /* Bytes of a page for these kv_heads, head_dim and page_tokens (nothing else of desc is read); negative if they are not valid. */
 int64_t st_attn_page_bytes(const st_attn_desc* desc);
-/* Validates the descriptors, divides the work by what they allow at most (max_new, table_pages), uploads the tables and allocates the
- * workspace.  A pointer may be NULL that none of the calls made with the plan needs.  opts: host_only is read, and split_k (> 0:
- * into how many parts each long sequence's tokens are divided, where they are). */
+/* Validates the descriptors, divides the work by what they allow at most (max_new, max_tokens, table_pages) and, within that, on the device by
+ * the lengths that there are, uploads the tables and allocates the workspace.  A pointer may be NULL that none of the calls made with the
+ * plan needs.  opts: host_only is read, and split_k (> 0: into how many parts the tokens that a row sees are divided; at most 64 are, 16 where
+ * max_new * heads / kv_heads is above 32).
+ * max_new decides how a tenant's work is divided: up to 32 rows of a key head go over a sequence's tokens together, more take workgroups of
+ * their own.  Sequences of one new token among prompts belong in a descriptor of their own: two tenants of a plan may read one pool, and
+ * append to different pages of it.
+ * ST_ERR_UNSUPPORTED: more than 2^16 heads, rows more than 2^32 elements apart; a page of 2^31 bytes, 2^30 tokens (of a table or a sequence's
+ * rows), 2^24 sequences, 2^23 workgroups or more of them. */
 st_status st_attn_plan(const st_attn_desc* descs, int32_t n_tenants, const st_plan_opts* opts, st_attn** out_plan);
 /* New tokens' keys and values (k, v) into the cache.  Two sequences that share a page must not both write to it. */
 st_status st_attn_append(const st_attn* plan, void* hip_stream);
