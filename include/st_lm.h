@@ -153,9 +153,9 @@ int64_t st_attn_page_bytes(const st_attn_desc* desc);
 /* Validates the descriptors, divides the work by what they allow at most (max_new, max_tokens, table_pages) and, within that, on the device by
  * the lengths that there are, uploads the tables and allocates the workspace.  A pointer may be NULL that none of the calls made with the
  * plan needs.  opts: host_only is read, and split_k (> 0: into how many parts the tokens that a row sees are divided; at most 64 are, 16 where
- * max_new * heads / kv_heads is above 32).
- * max_new decides how a tenant's work is divided: up to 32 rows of a key head go over a sequence's tokens together, more take workgroups of
- * their own.  Sequences of one new token among prompts belong in a descriptor of their own: two tenants of a plan may read one pool, and
+ * there are many rows).
+ * max_new decides how a tenant's work is divided: where max_new * heads / kv_heads is up to 128 (64 with heads of 256) a workgroup's wavefronts go over a
+ * sequence's tokens for the same rows, else each has rows of its own.  Sequences of one new token among prompts belong in a descriptor of their own: two tenants of a plan may read one pool, and
  * append to different pages of it.
  * ST_ERR_UNSUPPORTED: more than 2^16 heads, rows more than 2^32 elements apart; a page of 2^31 bytes, 2^30 tokens (of a table or a sequence's
  * rows), 2^24 sequences, 2^23 workgroups or more of them. */

@@ -94,10 +94,13 @@ int most_steps(const st_attn_desc& d) {      // that a row tile of single tokens
   if (d.window) tokens = std::min(tokens, (int64_t)d.window + d.max_new + kAttnStep);
   return cdiv(tokens, kAttnStep) + 1;
 }
-// Few rows: the tokens are divided among wavefronts and workgroups; else the rows are.
+// Few rows: the tokens are divided among wavefronts and workgroups, for 32 rows at a time (16 with heads of 256); else the rows are.  Four times over
+// the widening costs less than wavefronts without rows (one sequence of 8192, 8 and 47 of 4096; us by tokens and by rows): 64 rows of heads
+// of 128 19.6 and 44, 24.6 and 46, 92 and 201; 128 rows 18.4 and 44, 30 and 46, 171 and 204; 192 33 and 45, but 57 and 47, 254
+// and 210.  Heads of 256: 64 rows 21.6 and 64, 30.5 and 53, 132 and 185; 128 rows 22 and 65, 43 and 54, but 260 and 189.
 int kind_of(const st_attn_desc& d) {
   const int rows = most_rows(d);
-  return rows <= 16 ? kAttnTokens1 : rows <= 32 ? kAttnTokens2 : kAttnRows;
+  return rows <= 16 ? kAttnTokens1 : rows <= (d.head_dim == 256 ? 64 : 128) ? kAttnTokens2 : kAttnRows;
 }
 
 // Workgroups that move a sequence's new tokens.
