@@ -126,7 +126,8 @@ bool find_rows(const st_attn_desc& d, int64_t row_tiles) { return kind_of(d) == 
 // Rows whose tokens are divided.  A stretch's tile of tokens takes some 1.7 us, and 2.9 where two workgroups share a compute unit (one does
 // with heads of 256: 1.3); the last workgroup reads each stretch's sums in 2.8 us (5.5): sqrt(root tiles) stretches take least time, as
 // far as there is room for them.  Either one workgroup to a compute unit, or two, if that makes nearly twice as many stretches.  Between one and
-// two the chip is filled unevenly, and many short stretches even that out.  In us, whole and divided (heads 32 and 8 of 128): 512 new tokens of
+// two the chip is filled unevenly, and many short stretches even that out; so they do where lengths differ, if they are long (heads 16 and 2 of
+// 256, 3000 of 8192 537 and 489 us; 1500 342 and 295), but not where one round of equal ones is just full.  In us, whole and divided (heads 32 and 8 of 128): 512 new tokens of
 // 16384 430 and 159 (in 5), of 4096 112 and 58 (5), 128 of 8192 215 and 50 (9), 64 of 32768 843 and 89 (16), 2048 of 8192 304 and 254 (5).
 constexpr int kMostRowSplit = 16;
 void row_stretches(AttnDev& T, const st_attn_desc& d, double tiles, int most_steps) {
@@ -136,7 +137,10 @@ void row_stretches(AttnDev& T, const st_attn_desc& d, double tiles, int most_ste
   T.want = std::min(one, kMostRowSplit);
   T.most = std::min(two > 1.8 * one ? two : one, kMostRowSplit);
   if (tiles > kNumCUs && tiles < 1.6 * kNumCUs && d.head_dim != 256) T.want = 3, T.most = 5;
-  T.split = most_steps <= T.whole ? 1 : std::max(1, std::min(T.most, (int)(std::sqrt((double)most_steps * T.root) + 1.0)));
+  const double places = kNumCUs * (d.head_dim == 256 ? 1 : 2);
+  T.least = tiles < 0.8 * places || (tiles > places && tiles < 2 * places) ? 4 : 1;
+  const int room = std::min(std::max(T.most, T.want), (int)(std::sqrt((double)most_steps * T.root) + 1.0));
+  T.split = most_steps <= T.whole ? 1 : std::max({1, room, std::min(T.least, most_steps / kAttnLevelSteps)});
 }
 
 st_status upload(st_attn* p) {
@@ -213,12 +217,14 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
     if (d.n_seqs == 0 || d.max_tokens == 0) continue;
     const int steps = most_steps(d);
     if (kind_of(d) != kAttnRows) {
-      // A stretch on every compute unit: more of them only cost their set-up and their joining (one context of 131072, us with 24, 32, 64
-      // stretches: 35.3, 36.9, 42.9; 32 of 8000 with heads of 256, 128, 256, 512 workgroups: 43.1, 28.4, 36.3).  But none longer
-      // than 192 steps, or a few long sequences outlast the others (64 of up to 8192: 75.5 us in one stretch each, 66.9 in two),
+      // A stretch on every compute unit, not one more: that would share its unit with another (single tokens of 5, 10 and 20 sequences of 8192 in
+      // 240 workgroups 16.2, 21.7 us and 160 38.2, in 280 to 320 20.4, 27.7, 44.8; 32 of 8000 with heads of 256, 128, 256, 512 workgroups:
+      // 43.1, 28.4, 36.3), and more of them cost their set-up and their joining (one context of 131072 with 24, 32, 64 stretches: 35.3, 36.9, 42.9).  But none longer
+      // than 192 steps where there are more sequences' heads than units, or a few long ones outlast the others (64 of up to 8192: 75.5 us in one
+      // stretch each, 66.9 in two),
       // and short ones whole (a single sequence of 1000: 8.2 us whole, 9.1 in two; of 2000: 12.0 whole, 9.5 in four; of 4000: 19.9, 9.9 in eight).
-      T.want = std::max(1, std::min(kAttnMaxSplit, (int)std::ceil(kNumCUs / tiles)));
-      T.whole = 40; T.most = 192; T.least = 2 * kAttnTokenWaves;
+      T.want = std::max(1, std::min(kAttnMaxSplit, (int)(kNumCUs / tiles)));
+      T.whole = 40; T.most = tiles > kNumCUs ? 192 : 8 * 192; T.least = 2 * kAttnTokenWaves;
       if (o.split_k > 0) T.want = std::min(o.split_k, kAttnMaxSplit), T.whole = 0, T.most = 1 << 30, T.least = 1;
       // ... as far as the table has no more room than is used: 2048 workgroups in all, as those of stretches that there are not take time, too
       const int parts = std::max(T.want, std::min({kAttnMaxSplit, cdiv(steps, T.most), (int)std::max(1.0, 2048 / tiles)}));
@@ -227,7 +233,7 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
       T.chunk = std::max(T.least, cdiv(steps, T.split));
     } else {
       row_stretches(T, d, row_tiles, steps / (attn_row_tokens(d.head_dim) / kAttnStep) + 2);
-      if (o.split_k > 0) T.split = T.want = T.most = std::min(o.split_k, kMostRowSplit), T.root = 1e12f, T.whole = 0;
+      if (o.split_k > 0) T.split = T.want = T.most = std::min(o.split_k, kMostRowSplit), T.root = 1e12f, T.whole = 0, T.least = 1;
     }
     n_items += find_rows(d, T.row_tiles) ? all_row_tiles(d) * d.kv_heads * T.split + 1 : (int64_t)d.n_seqs * d.kv_heads * T.row_tiles * T.split;
     n_moves += find_moves(d) ? all_moves(d) + 1 : d.n_seqs * move_parts(d);

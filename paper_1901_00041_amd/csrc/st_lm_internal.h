@@ -56,7 +56,7 @@ constexpr int kAttnStep = 32;            // tokens per step of a wavefront
 constexpr int kAttnTokenWaves = 8;
 constexpr int attn_row_waves(int dim) { return dim == 256 ? 8 : 4; }
 constexpr int attn_row_tokens(int dim) { return dim == 256 ? 32 : 64; }      // of a tile that they widen together
-constexpr int kAttnMaxSplit = 64;
+constexpr int kAttnMaxSplit = 64, kAttnLevelSteps = 48;
 constexpr int kAttnTokens1 = 0, kAttnTokens2 = 1, kAttnRows = 2, kAttnRowsSplit = 3, kNumAttnKinds = 4;      // RowsSplit: its tokens are divided, too
 // R of a kind: rows are as many as the registers hold beside their queries, scores and outputs
 constexpr int attn_blocks(int kind, int dim) { return kind == kAttnTokens1 ? 1 : kind == kAttnTokens2 ? (dim == 256 ? 1 : 2) : dim == 64 ? 4 : dim == 128 ? 3 : 1; }
@@ -95,7 +95,7 @@ struct AttnDev {
   int32_t least;         // so few that none but the last has fewer than these, and
   int32_t chunk;         // none has more than these.
   float root;            // With kAttnRowsSplit (a step: a tile of the workgroup): one up to `whole` steps, else the square root of root times the
-                         // steps, if that is `most` or more just these, else not more than `want`
+                         // steps, if that is `most` or more just these, else not more than `want`; but one per kAttnLevelSteps up to `least`
   uint32_t flip;         // sign bits of two query elements, where scale is negative
   int32_t pad[3];
 };
