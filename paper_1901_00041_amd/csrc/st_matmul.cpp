@@ -78,19 +78,20 @@ void set_pointers(MatmulDev& T, const st_matmul_desc& d, const st_matmul_desc& p
 
 // ---- choice of a tile shape and of a division of the reduction -----------------------------------------------------------
 // Microseconds of a launch of one shape: a workgroup alone takes first + steps step, a compute unit through which many pass busy_first +
-// steps busy_step for each; a divided reduction adds join and join_kb for each KiB of the tile's partial sums (and busy_kb per KiB of a
-// slice); the operands come at 5 TB/s.  The largest of the three is the time, the others weigh a little.  Constants fitted to 193
-// products of 1 to 4096 rows, 64 to 8192 outputs and inputs and 1 to 16 tenants, each measured with every shape and up to seven
-// divisions: what it picks takes 1.5 % longer in the geometric mean than the fastest of them.  [shape][fp32]
-struct Cost { double first, step, busy_first, busy_step, join, join_kb, busy_kb; };
+// steps busy_step for each, some way towards whole rounds; a step costs `rough` more where rows are no multiple of 16 bytes; a divided reduction
+// adds join and join_kb for each KiB of the tile's partial sums (and busy_kb per KiB of a slice); the operands come at 5 TB/s.  The largest of
+// the three is the time, the others weigh a little.  Constants fitted to 523 products of 1 to 4096 rows, 64 to 8192 outputs and inputs, odd sizes among them, and
+// 1 to 16 tenants, each measured with every shape and up to seven divisions: what it picks takes 0.8 % longer in the geometric mean
+// than the fastest of them (2.3 % on 150 others).  [shape][fp32]
+struct Cost { double first, step, busy_first, busy_step, join, join_kb, busy_kb, rounds, rough; };
 constexpr Cost kCosts[kNumMatmulShapes][2] = {
-    {{3.36, 1.23, 16.2, 1.52, 6.98, 0.0619, 0.0383}, {8.18, 15.7, 0.0289, 9.24, 1.9e-05, 0.00505, 0.128}},
-    {{4.85, 0.511, 3.59, 0.521, 8.86, 0.0166, 0.0742}, {38.6, 0.806, 0.393, 1.4, 4.33, 0.0135, 0.268}},
-    {{0.925, 0.195, 0.975, 0.296, 1.13, 0.0111, 0.131}, {1.09, 0.415, 2.01, 0.487, 1.2, 0.0104, 0.0732}},
-    {{3.84, 0.145, 1.48, 1.23, 0.707, 0.0756, 0.119}, {6.19, 0.468, 1.23, 1.36, 1.06, 0.00445, 4.56e-09}},
-    {{1.23, 0.315, 0.527, 0.501, 0.347, 0.0287, 0.901}, {2.85, 0.109, 0.949, 1.23, 1.22, 0.0207, 5.71e-09}},
-    {{0.896, 0.22, 0.731, 0.394, 0.964, 0.0708, 0.471}, {1.55, 0.153, 0.768, 0.541, 1.23, 0.106, 4.4e-08}},
-    {{1.02, 0.0846, 1.3, 0.179, 0.551, 0.198, 0.703}, {1.73, 0.0781, 2.17, 0.0348, 0.793, 0.213, 0.0953}},
+    {{6.68, 0.797, 11.4, 1.3, 2.12, 0.0264, 0.0284, 0.425, 0.33}, {49.5, 26.1, 6.17, 0.758, 1.31, 0.0335, 0.0125, 1, 0.0134}},
+    {{2.85, 0.531, 2.83, 0.441, 2.86, 0.00758, 0.0625, 0.494, 0.407}, {10.1, 1.15, 8.61, 1.61, 0.839, 0.00454, 0.0239, 0.312, 0.156}},
+    {{0.886, 0.16, 1.06, 0.187, 1.45, 0.0124, 0.113, 0.758, 0.455}, {0.31, 0.562, 2.34, 0.446, 1.22, 0.0206, 0.0923, 1, 0.184}},
+    {{12.2, 2.1, 3.21, 5.75, 6.99, 0.806, 0.00838, 0.431, 6.61}, {3.47, 0.329, 0.0943, 1.2, 0.784, 0.018, 0.0826, 1, 0.0131}},
+    {{1.61, 0.112, 0.592, 0.794, 0.651, 0.0436, 0.238, 1, 3.13}, {4.09, 0.117, 0.333, 0.449, 0.772, 0.0156, 0.141, 1, 0.0545}},
+    {{0.528, 0.231, 0.526, 0.326, 0.283, 0.0599, 0.522, 1, 0.731}, {0.139, 0.196, 0.472, 0.413, 0.52, 0.203, 0.0831, 0.661, 0.0649}},
+    {{0.655, 0.1, 2, 0.108, 0.375, 0.194, 0.489, 0.831, 0.53}, {1.24, 0.0904, 1.78, 0.145, 0.7, 0.241, 0.213, 1, 0.00079}},
 };
 constexpr double kLaunchUs = 2.0;      // ... and what a launch takes beside them
 constexpr int kMostSplit = 32;
@@ -109,9 +110,11 @@ double time_of(const st_matmul_desc& d, int shape, int split, double share) {
   const bool f32 = d.in_dtype == ST_DT_F32;
   const Cost& c = kCosts[shape][f32];
   const int steps = std::max(1, cdiv(std::max(1, steps_of(d, shape)), split * (S.skinny ? 4 : 1)));
-  const double items = (double)cdiv(d.M, S.MT) * cdiv(d.N, S.NT) * split / (kNumCUs * share), kb = S.MT * S.NT * 4 / 1024.0;
-  const double alone = c.first + steps * c.step + (split > 1 ? c.join + c.join_kb * split * kb : 0.0);
-  const double busy = items * (c.busy_first + steps * c.busy_step + (split > 1 ? c.busy_kb * kb : 0.0));
+  double items = (double)cdiv(d.M, S.MT) * cdiv(d.N, S.NT) * split / (kNumCUs * share);
+  if (items > 1) items += c.rounds * (std::ceil(items) - items);
+  const double kb = S.MT * S.NT * 4 / 1024.0, rough = (int64_t)d.K * elem_size(d.in_dtype) % 16 != 0 ? 1 + c.rough : 1;
+  const double alone = c.first + steps * c.step * rough + (split > 1 ? c.join + c.join_kb * split * kb : 0.0);
+  const double busy = items * (c.busy_first + steps * c.busy_step * rough + (split > 1 ? c.busy_kb * kb : 0.0));
   const double memory = ((double)d.N * d.K + (double)d.M * d.K) * elem_size(d.in_dtype) / (5e6 * share), most = std::max(alone, busy);
   return std::max(most, memory) + 0.25 * std::min(alone, busy) + 0.3 * std::min(memory, most);
 }
