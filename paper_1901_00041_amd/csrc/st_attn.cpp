@@ -138,7 +138,7 @@ void row_stretches(AttnDev& T, const st_attn_desc& d, double tiles, int most_ste
   T.most = std::min(two > 1.8 * one ? two : one, kMostRowSplit);
   if (tiles > kNumCUs && tiles < 1.6 * kNumCUs && d.head_dim != 256) T.want = 3, T.most = 5;
   const double places = kNumCUs * (d.head_dim == 256 ? 1 : 2);
-  T.least = tiles < 0.8 * places || (tiles > places && tiles < 2 * places) ? 4 : 1;
+  T.least = tiles < 0.8 * places || (tiles > places && tiles < 1.6 * places) ? 3 : 1;
   const int room = std::min(std::max(T.most, T.want), (int)(std::sqrt((double)most_steps * T.root) + 1.0));
   T.split = most_steps <= T.whole ? 1 : std::max({1, room, std::min(T.least, most_steps / kAttnLevelSteps)});
 }

@@ -368,7 +368,8 @@ __device__ __forceinline__ int tokens_chunk(int steps, ConstAttn& T) {
 __device__ __forceinline__ int rows_chunk(int steps, ConstAttn& T) {
   if (steps <= T.whole) return steps;
   const int best = (int)(__builtin_amdgcn_sqrtf((float)steps * T.root) + 0.5f), few = best < T.want ? best : T.want, room = best >= T.most ? T.most : few;
-  const int level = steps / kAttnLevelSteps < T.least ? steps / kAttnLevelSteps : T.least, parts = room > level ? room : level;
+  const int level = steps / kAttnLevelSteps < T.least ? steps / kAttnLevelSteps : T.least, many = room > level ? room : level;
+  const int parts = many < T.split ? many : T.split;
   return parts > 1 ? (steps + parts - 1) / parts : steps;
 }
 

@@ -49,15 +49,16 @@ struct MatmulItem { uint32_t tenant, tile_m, tile_n, slice; };
 int launch_matmul(int dtype, int shape, const MatmulDev* table_dev, const MatmulItem* items_dev, int64_t n_items, void* stream);
 
 // ---- attention over a paged cache in 4 bits ---------------------------------------------------------------------------
-// How an st_attn_run divides the work (see st_attn.hip).  kByTokens: a workgroup's wavefronts take the tokens of a stretch in turn, all
-// for the same rows, of which there are 16 R; kByRows: each wavefront takes 16 R rows of its own and all the tokens they see.
+// How an st_attn_run divides the work (see st_attn.hip).  kAttnTokens1, 2: a workgroup's wavefronts take the tokens of a stretch in turn, all for
+// the same rows, of which there are 16 R; kAttnRows: each wavefront takes 16 R rows of its own and all the tokens they see, or (kAttnRowsSplit) a stretch of them.
 constexpr int kAttnBlock = 16;           // tokens per cache block
 constexpr int kAttnStep = 32;            // tokens per step of a wavefront
 constexpr int kAttnTokenWaves = 8;
 constexpr int attn_row_waves(int dim) { return dim == 256 ? 8 : 4; }
 constexpr int attn_row_tokens(int dim) { return dim == 256 ? 32 : 64; }      // of a tile that they widen together
-constexpr int kAttnMaxSplit = 64, kAttnLevelSteps = 48;
-constexpr int kAttnTokens1 = 0, kAttnTokens2 = 1, kAttnRows = 2, kAttnRowsSplit = 3, kNumAttnKinds = 4;      // RowsSplit: its tokens are divided, too
+constexpr int kAttnMaxSplit = 64;
+constexpr int kAttnLevelSteps = 48;      // a stretch of rows that levels out unlike lengths is as long as that: its joining is then a twentieth of it
+constexpr int kAttnTokens1 = 0, kAttnTokens2 = 1, kAttnRows = 2, kAttnRowsSplit = 3, kNumAttnKinds = 4;
 // R of a kind: rows are as many as the registers hold beside their queries, scores and outputs
 constexpr int attn_blocks(int kind, int dim) { return kind == kAttnTokens1 ? 1 : kind == kAttnTokens2 ? (dim == 256 ? 1 : 2) : dim == 64 ? 4 : dim == 128 ? 3 : 1; }
 
