@@ -124,23 +124,23 @@ int64_t all_row_tiles(const st_attn_desc& d) {
 bool find_rows(const st_attn_desc& d, int64_t row_tiles) { return kind_of(d) == kAttnRows && d.n_seqs * row_tiles > kAttnLoose * all_row_tiles(d); }
 
 // Rows whose tokens are divided.  A stretch's tile of tokens takes some 1.7 us, and 2.9 where two workgroups share a compute unit (one does
-// with heads of 256: 1.3); the last workgroup reads each stretch's sums in 2.8 us (5.5): sqrt(root tiles) stretches take least time, as
+// with heads of 256: 2.2); the last workgroup reads each stretch's sums in 2.8 us (5.5): sqrt(root tiles) stretches take least time, as
 // far as there is room for them.  Either one workgroup to a compute unit, or two, if that makes nearly twice as many stretches.  Between one and
 // two the chip is filled unevenly, and many short stretches even that out; so they do where lengths differ, if they are long (heads 16 and 2 of
-// 256, 3000 of 8192 537 and 489 us; 1500 342 and 295), but not where one round of equal ones is just full.  In us, whole and divided (heads 32 and 8 of 128): 512 new tokens of
+// 256, 3000 of 8192 420 and 391 us; 1500 280 and 240), but not where one round of equal ones is just full.  In us, whole and divided (heads 32 and 8 of 128): 512 new tokens of
 // 16384 430 and 159 (in 5), of 4096 112 and 58 (5), 128 of 8192 215 and 50 (9), 64 of 32768 843 and 89 (16), 2048 of 8192 304 and 254 (5).
 constexpr int kMostRowSplit = 16;
 void row_stretches(AttnDev& T, const st_attn_desc& d, double tiles, int most_steps) {
   const int one = std::max(1, (int)(kNumCUs / tiles)), two = d.head_dim == 256 ? one : std::max(1, (int)(2 * kNumCUs / tiles));
-  T.root = d.head_dim == 256 ? 0.24f : 0.62f;
-  T.whole = d.head_dim == 256 ? 20 : 8;
+  T.root = d.head_dim == 256 ? 0.4f : 0.62f;
+  T.whole = d.head_dim == 256 ? 10 : 8;
   T.want = std::min(one, kMostRowSplit);
   T.most = std::min(two > 1.8 * one ? two : one, kMostRowSplit);
   if (tiles > kNumCUs && tiles < 1.6 * kNumCUs && d.head_dim != 256) T.want = 3, T.most = 5;
   const double places = kNumCUs * (d.head_dim == 256 ? 1 : 2);
   T.least = tiles < 0.8 * places || (tiles > places && tiles < 1.6 * places) ? 3 : 1;
   const int room = std::min(std::max(T.most, T.want), (int)(std::sqrt((double)most_steps * T.root) + 1.0));
-  T.split = most_steps <= T.whole ? 1 : std::max({1, room, std::min(T.least, most_steps / kAttnLevelSteps)});
+  T.split = most_steps <= T.whole ? 1 : std::max({1, room, std::min(T.least, most_steps / attn_level_steps(d.head_dim))});
 }
 
 st_status upload(st_attn* p) {
@@ -232,7 +232,7 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
       T.want = std::min(T.want, T.split);
       T.chunk = std::max(T.least, cdiv(steps, T.split));
     } else {
-      row_stretches(T, d, row_tiles, steps / (attn_row_tokens(d.head_dim) / kAttnStep) + 2);
+      row_stretches(T, d, row_tiles, steps / (kAttnRowTokens / kAttnStep) + 2);
       if (o.split_k > 0) T.split = T.want = T.most = std::min(o.split_k, kMostRowSplit), T.root = 1e12f, T.whole = 0, T.least = 1;
     }
     n_items += find_rows(d, T.row_tiles) ? all_row_tiles(d) * d.kv_heads * T.split + 1 : (int64_t)d.n_seqs * d.kv_heads * T.row_tiles * T.split;

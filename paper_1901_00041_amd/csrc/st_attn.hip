@@ -365,10 +365,11 @@ __device__ __forceinline__ int tokens_chunk(int steps, ConstAttn& T) {
   const int chunk = even > T.least ? even : T.least;
   return chunk < T.chunk ? chunk : T.chunk;
 }
+template <int D>
 __device__ __forceinline__ int rows_chunk(int steps, ConstAttn& T) {
   if (steps <= T.whole) return steps;
   const int best = (int)(__builtin_amdgcn_sqrtf((float)steps * T.root) + 0.5f), few = best < T.want ? best : T.want, room = best >= T.most ? T.most : few;
-  const int level = steps / kAttnLevelSteps < T.least ? steps / kAttnLevelSteps : T.least, many = room > level ? room : level;
+  const int level = steps / attn_level_steps(D) < T.least ? steps / attn_level_steps(D) : T.least, many = room > level ? room : level;
   const int parts = many < T.split ? many : T.split;
   return parts > 1 ? (steps + parts - 1) / parts : steps;
 }
@@ -398,21 +399,22 @@ __device__ __forceinline__ void store_out(ConstAttn& T, const Seq& S, int head, 
 }
 
 // ---- each wavefront its own rows ----------------------------------------------------------------------------------------
-// The wavefronts of a workgroup go through the same tokens, TT at a time.  Each of them widens a block of the next tile (or half of
-// one) into LDS, in operand order (fragment f, lane l at 16 bytes (64 f + l)), while all compute on the present one: two buffers, one
-// barrier a tile.  A wavefront issues a vector instruction every five to six clocks at best and its MFMAs take sixteen each, so the
-// widening is cut into pieces that are issued between MFMAs.
+// The wavefronts of a workgroup go through the same tokens, TT at a time.  Each of them widens a block of the next tile (or half of one)
+// into LDS, in operand order (fragment f, lane l at 16 bytes (64 f + l)), while all compute on the present one: two buffers, one barrier a
+// tile.  A wavefront issues a vector instruction every five to six clocks at best and its MFMAs take sixteen each, so the widening is cut
+// into pieces that are issued between MFMAs.  Fewer tokens to a tile cost more: the look-ups and addresses are a tile's (heads of 256, chunks of
+// 333 in windows, with 32 97.5 us, with 64 82.0).
 //
 // SPLIT: few rows over many tokens, which are divided into stretches.  A stretch's sums lie in memory as they lie in the lanes, and whoever
 // arrives last adds them up in order.
 template <int DT, int D, int R, bool SPLIT>
 __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel(const AttnDev* table, const AttnItem* items) {
   typedef Attend<DT, D, R, true> A;
-  constexpr int W = attn_row_waves(D), TT = attn_row_tokens(D), BLOCKS = TT / 16, KW = A::KW, NE = A::NE;
+  constexpr int W = attn_row_waves(D), TT = kAttnRowTokens, BLOCKS = TT / 16, KW = A::KW, NE = A::NE;
   constexpr int SHARE = W / BLOCKS;                                     // wavefronts to a block
   constexpr int KWAVE = KW / SHARE, VWAVE = NE / SHARE;                 // fragments that a wavefront makes of its block's keys and values
   constexpr int KF = BLOCKS * KW, VF = TT / 32 * NE;                    // fragments of a tile
-  static_assert(W % BLOCKS == 0 && (D == 256 ? SHARE == 4 : SHARE == 1) && (KWAVE == 2 || KWAVE == 4), "a part is whole fragments, and lies in one word of a token's codes");
+  static_assert(W % BLOCKS == 0 && (D == 256 ? SHARE == 2 : SHARE == 1) && (KWAVE == 2 || KWAVE == 4), "a part is whole fragments, and lies in one word of a token's codes");
   __shared__ __align__(16) u32x4 frags[2][KF + VF][64];
   __shared__ __align__(16) int hidden[2][BLOCKS];
   const ConstAttnItem& ci = ((ConstAttnItem*)items)[blockIdx.x];
@@ -434,7 +436,7 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
   int n0 = all.lo / TT, n1 = all.hi >= all.lo ? all.hi / TT + 1 : n0, active = 1;
   if constexpr (SPLIT) {      // stretches as long as those of the sequence's last rows, so that all take about as long
     const int most = T.window && T.window + ROWS < S.length ? T.window + ROWS : S.length;
-    const int chunk = rows_chunk((most + TT - 1) / TT + 1, T);
+    const int chunk = rows_chunk<D>((most + TT - 1) / TT + 1, T);
     active = n1 - n0 > chunk ? (n1 - n0 + chunk - 1) / chunk : 1;
     if (stretch >= active) return;
     if (active > 1) {
@@ -450,8 +452,8 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
   struct Raw { uint32_t k[KWAVE], v[4], ks, vs; int page; };            // the part as it lies in the cache; v: a word per token (D = 64: per two)
   Raw raw;
   Table pages_of(T, seq, n0 < n1 ? n0 * TT : 0, n0 < n1 ? all.hi : 0, lane);
-  const uint32_t k_at = (uint32_t)(i * (D / 2) + g * (D / 8) + part * KWAVE * 4), v_at = (uint32_t)(8 * D + (i * 16 + 4 * g) * (D / 32) + part / 2 * 4);
-  const uint32_t ks_at = (uint32_t)(16 * D + i * (D / 32) + (D == 64 ? g / 2 : D == 128 ? g : 2 * g + part / 2));
+  const uint32_t k_at = (uint32_t)(i * (D / 2) + g * (D / 8) + part * KWAVE * 4), v_at = (uint32_t)(8 * D + (i * 16 + 4 * g) * (D / 32) + part * 4);
+  const uint32_t ks_at = (uint32_t)(16 * D + i * (D / 32) + (D == 64 ? g / 2 : D == 128 ? g : 2 * g + part));
   const uint32_t vs_at = (uint32_t)(16 * D + D / 2 + (D == 64 ? i / 8 : D == 128 ? i / 4 : i / 2) * 16 + 4 * g);
   auto look_up = [&](int n) __attribute__((always_inline)) {
     const int t = n * TT + kb * 16;
@@ -503,7 +505,7 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
       static_for<4>([&](auto X) {
         constexpr int t = decltype(X)::value;
         if constexpr (D == 64) c[t] = widen<DT, t % 2 * 2 + e2>(raw.v[t / 2], vsc[t]);
-        else c[t] = widen<DT, e2>(D == 128 ? raw.v[t] : raw.v[t] >> (part % 2 * 16), vsc[t]);
+        else c[t] = widen<DT, e2>(raw.v[t], vsc[t]);
       });
       u32x2* to = (u32x2*)&frags[buf][KF + kb / 2 * NE + part * VWAVE + 2 * e2][lane] + kb % 2;
       to[0] = u32x2{__builtin_amdgcn_perm(c[1], c[0], 0x05040100u), __builtin_amdgcn_perm(c[3], c[2], 0x05040100u)};

@@ -55,9 +55,9 @@ constexpr int kAttnBlock = 16;           // tokens per cache block
 constexpr int kAttnStep = 32;            // tokens per step of a wavefront
 constexpr int kAttnTokenWaves = 8;
 constexpr int attn_row_waves(int dim) { return dim == 256 ? 8 : 4; }
-constexpr int attn_row_tokens(int dim) { return dim == 256 ? 32 : 64; }      // of a tile that they widen together
+constexpr int kAttnRowTokens = 64;       // of a tile that they widen together
 constexpr int kAttnMaxSplit = 64;
-constexpr int kAttnLevelSteps = 48;      // a stretch of rows that levels out unlike lengths is as long as that: its joining is then a twentieth of it
+constexpr int attn_level_steps(int dim) { return dim == 256 ? 24 : 48; }      // a stretch of rows that levels out unlike lengths is as long as that: its joining is then a twentieth of it
 constexpr int kAttnTokens1 = 0, kAttnTokens2 = 1, kAttnRows = 2, kAttnRowsSplit = 3, kNumAttnKinds = 4;
 // R of a kind: rows are as many as the registers hold beside their queries, scores and outputs
 constexpr int attn_blocks(int kind, int dim) { return kind == kAttnTokens1 ? 1 : kind == kAttnTokens2 ? (dim == 256 ? 1 : 2) : dim == 64 ? 4 : dim == 128 ? 3 : 1; }
