@@ -224,7 +224,9 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
       // stretch each, 66.9 in two),
       // and short ones whole (a single sequence of 1000: 8.2 us whole, 9.1 in two; of 2000: 12.0 whole, 9.5 in four; of 4000: 19.9, 9.9 in eight).
       T.want = std::max(1, std::min(kAttnMaxSplit, (int)(kNumCUs / tiles)));
-      T.whole = 40; T.most = tiles > kNumCUs ? 192 : 8 * 192; T.least = 2 * kAttnTokenWaves;
+      const bool thirds = tiles > 0.5 * kNumCUs && 3 * tiles <= 2 * kNumCUs;      // 20 of 65536 in three 250 us, whole 272, in two 318; of 8192 36, 39, 45; of 2000 16.4, 14.5
+      if (thirds) T.want = 3;
+      T.whole = thirds ? 128 : 40; T.most = tiles > kNumCUs ? 192 : 8 * 192; T.least = 2 * kAttnTokenWaves;
       if (o.split_k > 0) T.want = std::min(o.split_k, kAttnMaxSplit), T.whole = 0, T.most = 1 << 30, T.least = 1;
       // ... as far as the table has no more room than is used: 2048 workgroups in all, as those of stretches that there are not take time, too
       const int parts = std::max(T.want, std::min({kAttnMaxSplit, cdiv(steps, T.most), (int)std::max(1.0, 2048 / tiles)}));
