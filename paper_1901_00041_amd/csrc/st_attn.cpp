@@ -88,10 +88,12 @@ void set_pointers(AttnDev& T, const st_attn_desc& p) {
 }
 
 // ---- division of the work ---------------------------------------------------------------------------------------------
+// A window that the table has no room for hides nothing; left out, sums with it stay far below 2^31 on the device.
+int window_of(const st_attn_desc& d) { return d.window < (int64_t)d.table_pages * d.page_tokens ? d.window : 0; }
 int most_rows(const st_attn_desc& d) { return (int)((int64_t)d.max_new * (d.heads / d.kv_heads)); }
 int most_steps(const st_attn_desc& d) {      // that a row tile of single tokens can have to go through
   int64_t tokens = (int64_t)d.table_pages * d.page_tokens;
-  if (d.window) tokens = std::min(tokens, (int64_t)d.window + d.max_new + kAttnStep);
+  if (const int window = window_of(d)) tokens = std::min(tokens, (int64_t)window + d.max_new + kAttnStep);
   return cdiv(tokens, kAttnStep) + 1;
 }
 // Few rows: the tokens are divided among wavefronts and workgroups, for 32 rows at a time (16 with heads of 256); else the rows are.  Four times over
@@ -200,7 +202,7 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
     T.n_seqs = d.n_seqs; T.max_tokens = d.max_tokens; T.max_new = d.max_new; T.n_pages = d.n_pages;
     T.page_shift = __builtin_ctz((unsigned)d.page_tokens);
     T.page_bytes = page_bytes(d);
-    T.table_pages = d.table_pages; T.window = d.window; T.causal = (d.flags & ST_ATTN_CAUSAL) != 0;
+    T.table_pages = d.table_pages; T.window = window_of(d); T.causal = (d.flags & ST_ATTN_CAUSAL) != 0;
     // hidden tokens get the score -inf, which has to stay that under the scale: a negative one changes the queries' signs instead, and one of
     // 0, or so small, counts as 2^-100, under which all finite scores are equal, too
     T.scale = std::min(std::max(std::fabs(d.scale) * 1.44269504088896340736f, 7.888609e-31f), 3.0e38f);
