@@ -90,8 +90,9 @@ int32_t st_matmul_tile_count(void);
  * that the largest value is never cut off below 2^127; each x is divided by the scale and rounded to the nearest element, ties to the one with the
  * even code, at most 6.  A value that is not finite makes its token's head unreadable: all its scales become 255 (keys) and 1 (values),
  * all its codes 0; attention reads its key as not a number and its value as 0.
- * Attention takes keys and values in the descriptor's dtype, which holds all that is written from that type: bfloat16 any element under a scale of 2^-126 to 2^125, fp16
- * what it can represent (a scale above 2^13 counts as 2^13, values below 2^-24 are rounded).
+ * Attention takes keys and values in the descriptor's dtype: bfloat16 any element under a scale of 2^-126 to 2^125; fp16 any under a scale of up to 2^14, the
+ * largest that is written from that type (one above it counts as it), elements below 2^-22 as multiples of 2^-23.  fp16 outputs that would be above 65504 are 65504.
+ * st_attn_read gives every element as the nearest number of dtype, in fp16 65504 at most, and not a number for keys of an unreadable head.
  * A pool is n_pages pages of st_attn_page_bytes() bytes.  A page holds page_tokens tokens: for each key head in turn its
  * page_tokens / 16 blocks, each of 16 tokens t and head_dim + head_dim / 16 bytes a token:
  *   keys' codes     [t][head_dim / 2]          byte j holds elements 2j (lower half) and 2j + 1
@@ -125,7 +126,7 @@ typedef struct st_attn_desc {
   int32_t n_pages, page_tokens, table_pages;   /* page_tokens 16, 32, 64, ..., 1024                                         */
   int32_t window;            /* > 0 (causal only): a token sees itself and the window - 1 tokens before it; 0: all           */
   uint32_t flags;            /* ST_ATTN_CAUSAL: token p sees tokens 0 .. p of its sequence; else all length[i] of them       */
-  float scale;               /* of the scores, before the softmax; finite; its size counts as 6e-31 at least, 2e38 at most   */
+  float scale;               /* of the scores, before the softmax; finite; its size counts as 6e-31 at least, 2e38 at most (fp16 1e38) */
   int32_t reserved;          /* must be 0                                                                                   */
   int64_t ldq, ldk, ldv, ldo; /* elements from a row to the next of q, k (and k_out), v (and v_out), out; 0 = dense          */
   const void* q;             /* [max_tokens][heads][head_dim], for st_attn_run                                              */

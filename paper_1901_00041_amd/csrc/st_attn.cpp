@@ -205,7 +205,8 @@ st_status build(st_attn* p, const st_attn_desc* descs, int n, const st_plan_opts
     T.table_pages = d.table_pages; T.window = window_of(d); T.causal = (d.flags & ST_ATTN_CAUSAL) != 0;
     // hidden tokens get the score -inf, which has to stay that under the scale: a negative one changes the queries' signs instead, and one of
     // 0, or so small, counts as 2^-100, under which all finite scores are equal, too
-    T.scale = std::min(std::max(std::fabs(d.scale) * 1.44269504088896340736f, 7.888609e-31f), 3.0e38f);
+    const float twice = d.dtype == ST_DT_F16 ? 2.f : 1.f;      // keys are widened under half their scale there (see kHalved in st_attn.hip)
+    T.scale = twice * std::min(std::max(std::fabs(d.scale) * 1.44269504088896340736f, 7.888609e-31f), 3.0e38f / twice);
     T.flip = d.scale < 0 ? 0x80008000u : 0u;
     T.row_tiles = cdiv(most_rows(d), (kind == kAttnRows ? attn_row_waves(d.head_dim) : 1) * 16 * attn_blocks(kind, d.head_dim));
     T.split = 1;

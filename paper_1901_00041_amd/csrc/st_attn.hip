@@ -108,16 +108,21 @@ __device__ __forceinline__ uint32_t widen(uint32_t codes, float scale) {      //
   if constexpr (DT == ST_DT_BF16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, BYTE));
   else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, BYTE));
 }
-// Scales above these count as these, so that no value is infinite (and weight 0 times it not a number).
-template <int DT> constexpr uint32_t kMostScale = DT == ST_DT_BF16 ? 252u : 140u;
+// fp16 ends at 65504, but a group whose largest value is above 49152 has the scale 2^14, under which the elements 4 and 6 are 65536 and 98304.
+// Attention therefore widens under half the scale, kHalved of it in all: scores are made up for by twice the factor behind them, outputs by the division
+// by the sum, both without a rounding.  What it costs: elements below 2^-22 become multiples of 2^-23.
+template <int DT> constexpr bool kHalved = DT == ST_DT_F16;
+// Scales above these (of another type, or memory that was never written) count as these, so that no value is infinite (and weight 0 times it not a number).
+template <int DT> constexpr uint32_t kMostScale = kHalved<DT> ? 141u : 252u;
 template <int DT>
 __device__ __forceinline__ float value_scale(uint32_t code) {
-  return __builtin_bit_cast(float, (code < kMostScale<DT> ? code : kMostScale<DT>) << 23);
+  const uint32_t held = code < kMostScale<DT> ? code : kMostScale<DT>;
+  return __builtin_bit_cast(float, kHalved<DT> ? ((held > 1u ? held : 1u) << 23) - (1u << 23) : held << 23);
 }
 template <int DT>
 __device__ __forceinline__ float key_scale(uint32_t code) {      // 255: not a number
-  const uint32_t held = code < kMostScale<DT> ? code : kMostScale<DT>;
-  return __builtin_bit_cast(float, code == 255u ? 0x7fc00000u : held << 23);
+  const float f = value_scale<DT>(code);
+  return code == 255u ? __builtin_bit_cast(float, 0x7fc00000u) : f;
 }
 
 template <int DT>
@@ -390,10 +395,22 @@ __device__ __forceinline__ Seen seen_by(ConstAttn& T, const Seq& S, int row0, in
   return s;
 }
 
+// One over a row's sum, and what the values' scales lack.
+template <int DT>
+__device__ __forceinline__ float inverse_of(float total) { return total == 0.f ? 0.f : (kHalved<DT> ? 2.f : 1.f) / total; }
+// W of a row's outputs: sums of its values, `inverse` for all of them.
 template <int DT, int W>
-__device__ __forceinline__ void store_out(ConstAttn& T, const Seq& S, int head, int row, int dim, int D, const float* v) {
+__device__ __forceinline__ void store_out(ConstAttn& T, const Seq& S, int head, int row, int dim, int D, const float* sums, float inverse) {
   const int j = row / T.group, h = row - j * T.group;
   uint16_t* p = (uint16_t*)T.out + (int64_t)(S.first + j) * T.ldo + (int64_t)(head * T.group + h) * D + dim;
+  float v[W];
+#pragma unroll
+  for (int e = 0; e < W; ++e) v[e] = sums[e] * inverse;
+  if constexpr (DT == ST_DT_F16) {      // of values that are 65536 in the cache; a row's outputs are all NaN or none is, by its sum, and a median with NaN alone is NaN
+    const float most = inverse == inverse ? 65504.f : inverse;
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = __builtin_amdgcn_fmed3f(v[e], -most, most);
+  }
   if constexpr (W == 8) *(u32x4_any*)p = u32x4{pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3]), pack_pair<DT>(v[4], v[5]), pack_pair<DT>(v[6], v[7])};
   else *(u32x2_any*)p = u32x2{pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3])};
 }
@@ -625,15 +642,15 @@ __global__ __launch_bounds__(attn_row_waves(D) * 64, 2) void st_attn_rows_kernel
   static_for<R>([&](auto J) {
     constexpr int r = decltype(J)::value;
     const int row = row0 + r * 16 + i;
-    const float total = a.row_sum(r), inv = total == 0.f ? 0.f : 1.f / total;
+    const float inv = inverse_of<DT>(a.row_sum(r));
     if (row < rows) {
       static_for<4>([&](auto X) {
         constexpr int x = decltype(X)::value;
         float v[D / 16];
-        static_for<D / 16>([&](auto E) { v[decltype(E)::value] = a.acc[decltype(E)::value][r][x] * inv; });
+        static_for<D / 16>([&](auto E) { v[decltype(E)::value] = a.acc[decltype(E)::value][r][x]; });
         const int dim = (4 * g + x) * (D / 16);
-        if constexpr (D == 64) store_out<DT, 4>(T, S, head, row, dim, D, v);
-        else static_for<D / 128>([&](auto C) { store_out<DT, 8>(T, S, head, row, dim + 8 * decltype(C)::value, D, v + 8 * decltype(C)::value); });
+        if constexpr (D == 64) store_out<DT, 4>(T, S, head, row, dim, D, v, inv);
+        else static_for<D / 128>([&](auto C) { store_out<DT, 8>(T, S, head, row, dim + 8 * decltype(C)::value, D, v + 8 * decltype(C)::value, inv); });
       });
     }
   });
@@ -690,7 +707,7 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
     float total = 0.f;
     for (int w = 0; w < W; ++w) total += wave_l[w][tid];
     wave_l[0][tid] = total;
-    inverse[tid] = total == 0.f ? 0.f : 1.f / total;
+    inverse[tid] = inverse_of<DT>(total);
   }
   const int64_t tile = ((int64_t)seq * T.kv_heads + head) * T.row_tiles + row_tile;
   const int64_t slots = (int64_t)T.n_seqs * T.kv_heads * T.row_tiles * T.split;
@@ -715,9 +732,8 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
       const int dim = c / EP * (D / 16) + pass * EP + c % EP;
       if (row0 + row < row1) {
         if (active == 1) {
-          const float f = inverse[row];
-          const float o[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
-          store_out<DT, 4>(T, S, head, row0 + row, dim, D, o);
+          const float o[4] = {v[0], v[1], v[2], v[3]};
+          store_out<DT, 4>(T, S, head, row0 + row, dim, D, o, inverse[row]);
         } else {
           const __amdgpu_buffer_rsrc_t rs = make_rsrc(parts + (int64_t)stretch * (ROWS * D), ROWS * D * 4);
           __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, (row * D + dim) * 4, 0, kAuxDeviceCoherent);
@@ -764,7 +780,7 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
       weight[s][tid] = w;
       total += w * sums[s * ROWS + tid];
     }
-    inverse[tid] = total == 0.f ? 0.f : 1.f / total;
+    inverse[tid] = inverse_of<DT>(total);
   }
   __syncthreads();
   // Four outputs to a thread.  Where that leaves threads over, they share the stretches: group k takes stretches k, k + groups, ...
@@ -795,9 +811,8 @@ __global__ __launch_bounds__(kAttnTokenWaves * 64, D <= 128 && R == 1 ? 4 : 2) v
         for (int k = 1; k < groups; ++k) v += shared[k * vectors + tid];
     }
     if (mine && group == 0) {
-      const float f = inverse[row];
-      const float o[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
-      store_out<DT, 4>(T, S, head, row0 + row, dim, D, o);
+      const float o[4] = {v[0], v[1], v[2], v[3]};
+      store_out<DT, 4>(T, S, head, row0 + row, dim, D, o, inverse[row]);
     }
   }
 }
@@ -833,6 +848,9 @@ __device__ __forceinline__ void encode8(const u32x4 in, uint32_t& codes, uint32_
   });
   codes = c;
 }
+
+// Of a pair of fp16 values, the infinite ones as the largest number of their sign.
+__device__ __forceinline__ uint32_t finite_pair(uint32_t p) { return p - ((p & 0x7fffu) == 0x7c00u ? 1u : 0u) - ((p & 0x7fff0000u) == 0x7c000000u ? 0x10000u : 0u); }
 
 template <int DT, int D, bool READ, int TURNS>
 __global__ __launch_bounds__(256) void st_attn_move_kernel(const AttnDev* table, const AttnItem* items) {
@@ -906,9 +924,18 @@ __global__ __launch_bounds__(256) void st_attn_move_kernel(const AttnDev* table,
         uint32_t vc;
         if constexpr (D == 64) vc = *(const uint16_t*)vp | (uint32_t)*(const uint16_t*)(vp + 32) << 16;
         else vc = *(const uint32_t*)vp;
-        const float kf = key_scale<DT>(*(const uint8_t*)ks), vf = value_scale<DT>(*(const uint8_t*)vs);
+        // whole scales here, the largest one that is written at most; fp16: what is infinite under them is the largest number
+        const uint32_t kb = *(const uint8_t*)ks, vb = *(const uint8_t*)vs, most = 252u;
+        const float kf = __builtin_bit_cast(float, kb == 255u ? 0x7fc00000u : (kb < most ? kb : most) << 23), vf = __builtin_bit_cast(float, (vb < most ? vb : most) << 23);
         k[n] = u32x4{widen<DT, 0>(kc, kf), widen<DT, 1>(kc, kf), widen<DT, 2>(kc, kf), widen<DT, 3>(kc, kf)};
         v[n] = u32x4{widen<DT, 0>(vc, vf), widen<DT, 1>(vc, vf), widen<DT, 2>(vc, vf), widen<DT, 3>(vc, vf)};
+        if (DT == ST_DT_F16 && __builtin_expect(__any((kb > vb ? kb : vb) > 140u) != 0, 0)) {
+          static_for<4>([&](auto X) {
+            constexpr int x = decltype(X)::value;
+            k[n][x] = finite_pair(k[n][x]);
+            v[n][x] = finite_pair(v[n][x]);
+          });
+        }
       }
       const int64_t row = S.first + j[n];
       *(u32x4_any*)((uint16_t*)T.k_out + row * T.ldk + head[n] * D + c * 8) = k[n];

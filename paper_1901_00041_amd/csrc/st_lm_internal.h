@@ -87,7 +87,7 @@ struct AttnDev {
   int32_t heads, kv_heads, group, n_seqs;
   int32_t max_tokens, max_new, n_pages, page_shift;
   int32_t table_pages, window, causal;
-  float scale;           // its size times log2(e), above zero
+  float scale;           // its size times log2(e), above zero; fp16: twice that
   int32_t row_tiles;     // per sequence and key head
   int32_t split;         // at most so many stretches.  How many, of wavefronts that take turns:
   int32_t whole;         // one for no more steps than these, else

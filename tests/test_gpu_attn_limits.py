@@ -1,9 +1,10 @@
 """Attention over caches in 4 bits (st_attn_*) at the ends of what its descriptors allow; formula, oracle and tolerances as in test_gpu_attn."""
+import numpy as np
 import pytest
 
 from paper_1901_00041_amd import st_conv as sc
 from paper_1901_00041_amd import st_lm
-from tests.attn_helpers import Tenant
+from tests.attn_helpers import Tenant, decode
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,90 @@ def test_a_window_as_long_as_the_table_hides_nothing(kind, dim, dtype):
         t.check_out(f"window {window}")
         assert torch.equal(whole.view(torch.int16), t.d["out"].view(torch.int16)), window
         assert st_lm.st_attn_status(plan) == bad == (st_lm.ST_ATTN_BAD_LENGTH if any(n > length for n, length in seqs) else 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_what_the_cache_gives_back_of_every_value(dim, dtype):
+    """All bit patterns of the type, by value: the elements that were written, each in the type, none beyond its largest number."""
+    torch = torch_()
+    heads = 4096 // dim
+    t = Tenant(heads, heads, dim, dtype, [(16, 16)], page=16, filled=False)
+    every = torch.arange(65536, dtype=torch.int32).to(torch.uint16).view(t.tt).double().numpy()
+    finite = every[np.isfinite(every)]
+    t.k[0] = np.concatenate([finite, np.zeros(65536 - finite.size)]).reshape(t.k[0].shape)
+    t.v[0] = np.random.default_rng(7).permutation(t.k[0].ravel()).reshape(t.k[0].shape)      # large and small ones in one group
+    plan = st_lm.st_attn_plan([t.upload().desc()], keep=t)
+    st_lm.st_attn_append(plan)
+    st_lm.st_attn_read(plan)
+    torch.cuda.synchronize()
+    t.fill([16])
+    assert np.array_equal(t.d["pages"].cpu().numpy(), t.pool.bytes)
+    most = torch.finfo(t.tt).max
+    for name, held in zip(("k_out", "v_out"), t.held(0)):
+        want = torch.from_numpy(held.transpose(1, 0, 2)).clamp(-most, most).to(t.tt).double().numpy()
+        assert np.array_equal(t.outputs(name)[:16], want), name
+
+
+@pytest.mark.parametrize("seqs, split", [([(1, 90)], 0), ([(3, 300)], 0), ([(80, 200)], 1), ([(70, 900)], 4)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_large_fp16_values_keep_their_size(dim, seqs, split):
+    """Groups with a largest value above 49152, whose scale is 2^14: attention takes what the cache holds, 65536 among it."""
+    t = Tenant(4, 2, dim, "f16", seqs, page=16, filled=False, gain=1e-3)
+    rounded = lambda x: torch_().from_numpy(x).half().double().numpy()  # noqa: E731
+    for x in (t.k[0], t.v[0]):
+        x[:, :, ::32] = rounded(np.where(np.arange(x.shape[0])[:, None, None] % 2, 60000.0, -50000.0) + 0 * x[:, :, ::32])
+        x[:, :, 1::32] = 30000.0
+        x[:, :, 2::32] = -8192.0
+    t.fill([seqs[0][1]])
+    assert (t.held(0)[1] == 65536.0).any() and (t.held(0)[1] == 32768.0).any()
+    run(t, sc.plan_opts(split_k=split))
+    t.check_out()
+
+
+@pytest.mark.parametrize("seqs, split", [([(1, 1), (1, 40)], 0), ([(3, 3), (2, 50)], 0), ([(80, 200)], 1), ([(70, 900)], 4)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_fp16_outputs_end_at_the_largest_number(dim, seqs, split):
+    """Where all values are 60000, which the cache holds as 65536, and for keys of them that are not numbers."""
+    t = Tenant(4, 2, dim, "f16", seqs, page=16, filled=False)
+    for x in t.v:
+        x[:], x[:, 1] = 60000.0, -65504.0
+    t.k[-1][-1, 1, 5] = np.nan
+    t.fill([length for _, length in seqs])
+    run(t, sc.plan_opts(split_k=split))
+    want = np.full(t.outputs().shape, np.nan)
+    want[:t.first[-1], :2], want[:t.first[-1], 2:] = 65504.0, -65504.0
+    want[t.first[-1] - 1, 2:] = np.nan             # the last token sees itself
+    assert np.array_equal(t.outputs(), want, equal_nan=True)
+
+
+@pytest.mark.parametrize("seqs", [[(1, 1)], [(80, 80)]])
+def test_the_smallest_fp16_values(seqs):
+    """Elements below 2^-22 may become multiples of 2^-23, half of which is 2^-24; the others are as they were, and the outputs' own rounding
+    is of half a step, 2^-25, at most.  Every query sees tokens of the same values only."""
+    t = Tenant(2, 1, 64, "f16", seqs, page=16, filled=False)
+    t.v[0][:] = np.arange(64) * 2.0 ** -24
+    t.fill([seqs[0][1]])
+    run(t, sc.plan_opts(split_k=1))
+    off = np.abs(t.outputs()[:seqs[0][0]] - t.held(0)[1][0, 0])
+    assert off.max() <= 2.0 ** -24 + 2.0 ** -25 and off[..., 32:].max() <= 2.0 ** -25
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_every_scale_that_a_page_can_hold(dim, dtype):
+    """Also those that only another type writes: an element that the type has no number for is rounded to one, or is its largest."""
+    torch = torch_()
+    t = Tenant(1, 1, dim, dtype, [(254, 254)], page=256, filled=False)
+    code = np.tile(np.arange(16, dtype=np.uint8), dim // 16)[None]
+    for p in range(254):
+        scale = np.full((1, dim // 32), p + 1, np.uint8)
+        t.pool.write(t.table[0, 0], p, code, scale, code[:, ::-1], scale)
+    plan = st_lm.st_attn_plan([t.upload().desc()], keep=t)
+    st_lm.st_attn_read(plan)
+    torch.cuda.synchronize()
+    most = torch.finfo(t.tt).max
+    scale = np.minimum(np.arange(1, 255), 252)[:, None].repeat(dim // 32, 1)      # 2^125: the largest that anybody writes
+    for name, codes in (("k_out", code), ("v_out", code[:, ::-1])):
+        want = torch.from_numpy(decode(codes.repeat(254, 0), scale)).clamp(-most, most).to(t.tt).double().numpy()
+        assert np.array_equal(t.outputs(name)[:254, 0], want), name
