@@ -68,7 +68,8 @@ typedef struct st_matmul_tenant_info {
 typedef struct st_matmul st_matmul; /* opaque */
 
 /* Validates the descriptors, picks a tile shape and a division of the reduction per tenant, lists the work items and uploads
- * them.  Of opts (NULL: defaults) tile_cfg, split_k and host_only are read, as in st_conv_plan.
+ * them.  Of opts (NULL: defaults) tile_cfg, split_k and host_only are read, as in st_conv_plan; split_k as far as there are steps for it and a
+ * tile's partial sums take 2^30 bytes.
  * n_tenants = 0, or M = 0 everywhere, gives a plan whose runs do nothing.
  * ST_ERR_UNSUPPORTED: a row longer than 2^20 elements or rows further apart than 2^21; 2^23 workgroups or more. */
 st_status st_matmul_plan(const st_matmul_desc* descs, int32_t n_tenants, const st_plan_opts* opts, st_matmul** out_plan);

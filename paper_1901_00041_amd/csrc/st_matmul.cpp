@@ -95,6 +95,8 @@ constexpr Cost kCosts[kNumMatmulShapes][2] = {
 };
 constexpr double kLaunchUs = 2.0;      // ... and what a launch takes beside them
 constexpr int kMostSplit = 32;
+// A tile's partial sums are reached by offsets of 32 bits of which 2^31 stands for none: a division that is asked for makes no more slices than this many bytes hold.
+constexpr int64_t kMostPartialBytes = (int64_t)1 << 30;
 
 int steps_of(const st_matmul_desc& d, int shape) {
   const int bytes = kMatmulShapes[shape].skinny ? kMatmulUnitBytes : kMatmulStepBytes;
@@ -124,6 +126,8 @@ struct Choice { int shape, split, per_split; };
 // The division of the reduction that suits a tenant best in a shape, and its time.
 Choice divide(const st_matmul_desc& d, int shape, double share, int forced, double* time) {
   const int steps = std::max(1, steps_of(d, shape));
+  const MatmulShape& S = kMatmulShapes[shape];
+  if (forced) forced = (int)std::min<int64_t>(forced, kMostPartialBytes / (S.MT * S.NT * 4));
   Choice best = {shape, 1, steps};
   *time = -1;
   for (int want = forced ? forced : 1; want <= (forced ? forced : kMostSplit); ++want) {
