@@ -41,6 +41,8 @@ __device__ __forceinline__ Seq sequence(ConstAttn& T, int seq, bool reports) {  
   if (reports && (f0 != a || f1 != b || length != len || n != all || all > length)) atomicOr(T.status, (uint32_t)ST_ATTN_BAD_LENGTH);
   return {f0, n, length, length - all};
 }
+// The last token that its j-th new token sees; below 0 for none, which are those before the sequence's start.
+__device__ __forceinline__ int last_seen(ConstAttn& T, const Seq& S, int j) { return T.causal || S.before + j < 0 ? S.before + j : S.length - 1; }
 // Where max_new allows far more work than max_tokens, items are not listed for each sequence, which leaves most of them without any, but
 // as many as there can be at most in all (kAttnFind): the part-th of all parts belongs to the sequence that is found here, 64 sequences at a
 // time, and is that sequence's part-th then.  parts(n): of a sequence with n new tokens.  One more item (kAttnCheck) looks at every sequence's numbers.
@@ -201,7 +203,7 @@ struct Attend {
         constexpr int b = decltype(B)::value;
         q[r][b] = real ? *(const u32x4_any*)(p + 8 * b) ^ T.flip : u32x4{0u, 0u, 0u, 0u};
       });
-      pos[r] = T.causal ? S.before + j : S.length - 1;
+      pos[r] = last_seen(T, S, j);
     });
   }
   // the page of both blocks of step s; a block behind `last` takes the first one's
@@ -382,10 +384,10 @@ __device__ __forceinline__ int rows_chunk(int steps, ConstAttn& T) {
 // The tokens that rows [row0, row1) of a sequence see: any of them, and all of them.
 struct Seen { int lo, hi, all_lo, all_hi; };
 __device__ __forceinline__ Seen seen_by(ConstAttn& T, const Seq& S, int row0, int row1) {
-  const int p0 = S.before + row0 / T.group, p1 = S.before + (row1 - 1) / T.group;
+  const int j0 = row0 / T.group, j1 = (row1 - 1) / T.group, p0 = S.before + j0, p1 = S.before + j1;
   Seen s;
-  s.hi = T.causal ? p1 : S.length - 1;
-  s.all_hi = T.causal ? p0 : S.length - 1;
+  s.hi = last_seen(T, S, j1);
+  s.all_hi = last_seen(T, S, j0);
   s.lo = T.window && p0 - T.window + 1 > 0 ? p0 - T.window + 1 : 0;
   s.all_lo = T.window && p1 - T.window + 1 > 0 ? p1 - T.window + 1 : 0;
   if (T.n_pages == 0) {

@@ -4,7 +4,7 @@ import pytest
 
 from paper_1901_00041_amd import st_conv as sc
 from paper_1901_00041_amd import st_lm
-from tests.attn_helpers import Tenant, decode
+from tests.attn_helpers import Tenant, attend, decode
 
 pytestmark = pytest.mark.gpu
 
@@ -132,3 +132,23 @@ def test_every_scale_that_a_page_can_hold(dim, dtype):
     for name, codes in (("k_out", code), ("v_out", code[:, ::-1])):
         want = torch.from_numpy(decode(codes.repeat(254, 0), scale)).clamp(-most, most).to(t.tt).double().numpy()
         assert np.array_equal(t.outputs(name)[:254, 0], want), name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("seqs, split, max_new", [([(5, 1), (1, 0), (7, 3)], 0, None), ([(40, 20), (70, 70), (90, 1)], 1, None), ([(300, 40), (64, 0)], 1, None),
+                                                  ([(700, 600), (130, 1500), (300, 1)], 4, None), ([(60, 20), (2, 1)] + [(1, 30)] * 60, 1, 4096)])
+def test_new_tokens_before_a_sequences_start_see_nothing(seqs, split, max_new, dim, dtype):
+    """Without a causal mask, too: they get zeros, and the others see every token that there is."""
+    t = Tenant(4, 2, dim, dtype, seqs, page=16, causal=False, max_new=max_new)
+    plan = run(t, sc.plan_opts(split_k=split))
+    got = t.outputs()
+    for s, (n, length) in enumerate(seqs):
+        before = max(0, n - length)
+        mine = got[t.first[s]:t.first[s] + n]
+        assert np.array_equal(mine[:before], np.zeros_like(mine[:before])), f"sequence {s}"
+        if n > before:
+            want, tol = attend(t.q[t.first[s] + before:t.first[s] + n], *t.held(s), length - (n - before), t.scale, False, 0, t.bits)
+            assert (np.abs(mine[before:] - want) <= tol).all(), f"sequence {s}"
+    t.check_untouched("", "out")
+    assert st_lm.st_attn_status(plan) == st_lm.ST_ATTN_BAD_LENGTH
