@@ -75,7 +75,7 @@ typedef struct st_matmul st_matmul; /* opaque */
 st_status st_matmul_plan(const st_matmul_desc* descs, int32_t n_tenants, const st_plan_opts* opts, st_matmul** out_plan);
 st_status st_matmul_run(const st_matmul* plan, void* hip_stream);
 /* All tenants' pointers at once, in stream order (as st_conv_plan_rebind_all): x, w, bias, y and residual are taken from descs,
- * everything else in them is ignored. */
+ * everything else in them is ignored.  Captured into a graph it happens at each replay, after which the plan has these pointers until the next call. */
 st_status st_matmul_rebind_all(st_matmul* plan, const st_matmul_desc* descs, int32_t n_tenants, void* hip_stream);
 st_status st_matmul_get_info(const st_matmul* plan, st_matmul_plan_info* out);
 st_status st_matmul_get_tenant_info(const st_matmul* plan, int32_t tenant, st_matmul_tenant_info* out);
@@ -171,7 +171,7 @@ st_status st_attn_read(const st_attn* plan, void* hip_stream);
  * Scores, the softmax's maximum and sum, and the mixed values are held in fp32, weights are rounded to dtype before they
  * multiply values.  A query that sees no token gets zeros. */
 st_status st_attn_run(const st_attn* plan, void* hip_stream);
-/* All tenants' pointers at once, in stream order: the nine tensors and tables are taken from descs, everything else in them is ignored. */
+/* All tenants' pointers at once, as st_matmul_rebind_all: the ten tensors and tables are taken from descs, everything else in them is ignored. */
 st_status st_attn_rebind_all(st_attn* plan, const st_attn_desc* descs, int32_t n_tenants, void* hip_stream);
 /* Waits for the device, then *bits = the ST_ATTN_BAD_* that any run since the last call met; they are cleared. */
 st_status st_attn_status(st_attn* plan, int32_t* bits);

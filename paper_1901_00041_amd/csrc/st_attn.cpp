@@ -22,6 +22,7 @@ struct st_attn {
   bool can_append = true, can_read = true, can_run = true;      // every pointer is there that the call needs
   st_attn_info totals = {};
   int device = 0;
+  bool graphs_rebind = false;          // a graph may put other pointers into the device's table than the host's has
   char* d_arena = nullptr;             // the one device allocation: table, items, status, counters, partial results
   AttnDev* d_tenants = nullptr;
   AttnItem* d_items = nullptr;
@@ -375,10 +376,14 @@ extern "C" st_status st_attn_rebind_all(st_attn* plan, const st_attn_desc* descs
     return fail(ST_ERR_OUT_OF_MEMORY, "host allocation failed");
   }
   for (int t = 0; t < n_tenants; ++t) set_pointers(next[t], descs[t]);
-  if (n_tenants > 0 && std::memcmp(next.data(), plan->tenants.data(), next.size() * sizeof(AttnDev)) != 0 && plan->d_tenants) {
+  const bool same = n_tenants == 0 || std::memcmp(next.data(), plan->tenants.data(), next.size() * sizeof(AttnDev)) == 0;
+  if (plan->d_tenants) {
     OnDevice on(plan->device);
     ST_HIP(on.error);
-    ST_HIP((hipError_t)launch_poke(next.data(), (int64_t)(next.size() * sizeof(AttnDev)), plan->d_tenants, hip_stream));
+    bool captured = false;
+    ST_HIP(is_captured(hip_stream, &captured));
+    if (!same || captured || plan->graphs_rebind) ST_HIP((hipError_t)launch_poke(next.data(), (int64_t)(next.size() * sizeof(AttnDev)), plan->d_tenants, hip_stream));
+    plan->graphs_rebind |= captured;
   }
   plan->tenants.swap(next);
   plan->can_append = append; plan->can_read = read; plan->can_run = run;

@@ -24,6 +24,14 @@ struct OnDevice {
   OnDevice& operator=(const OnDevice&) = delete;
 };
 
+// Whether what is queued on a stream becomes part of a graph.
+inline hipError_t is_captured(void* hip_stream, bool* captured) {
+  hipStreamCaptureStatus now = hipStreamCaptureStatusNone;
+  const hipError_t e = hip_stream ? hipStreamIsCapturing((hipStream_t)hip_stream, &now) : hipSuccess;      // the default stream cannot be
+  *captured = now != hipStreamCaptureStatusNone;
+  return e;
+}
+
 // A launch holds fewer than 2^32 threads, which its largest workgroups of 512 reach with this many.
 constexpr int64_t kMostWorkgroups = (int64_t)1 << 23;
 

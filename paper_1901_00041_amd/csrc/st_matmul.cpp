@@ -22,6 +22,7 @@ struct st_matmul {
   std::vector<MatmulItem> items;       // of all launches, one after another
   st_matmul_plan_info totals = {};
   int device = 0;
+  bool graphs_rebind = false;          // a graph may put other pointers into the device's table than the host's has
   char* d_arena = nullptr;             // the one device allocation: table, items, counters, partial tiles
   MatmulDev* d_tenants = nullptr;
   MatmulItem* d_items = nullptr;
@@ -359,11 +360,15 @@ extern "C" st_status st_matmul_rebind_all(st_matmul* plan, const st_matmul_desc*
     return fail(ST_ERR_OUT_OF_MEMORY, "host allocation failed");
   }
   for (int t = 0; t < n_tenants; ++t) set_pointers(next[t], plan->descs[t], descs[t]);
-  if (n_tenants == 0 || std::memcmp(next.data(), plan->tenants.data(), next.size() * sizeof(MatmulDev)) == 0) return ST_OK;
+  const bool same = n_tenants == 0 || std::memcmp(next.data(), plan->tenants.data(), next.size() * sizeof(MatmulDev)) == 0;
   if (!plan->totals.host_only && plan->d_tenants) {
     OnDevice on(plan->device);
     ST_HIP(on.error);
+    bool captured = false;
+    ST_HIP(is_captured(hip_stream, &captured));
+    if (same && !captured && !plan->graphs_rebind) return ST_OK;
     ST_HIP((hipError_t)launch_poke(next.data(), (int64_t)(next.size() * sizeof(MatmulDev)), plan->d_tenants, hip_stream));
+    plan->graphs_rebind |= captured;
   }
   plan->tenants.swap(next);
   for (int t = 0; t < n_tenants; ++t) {

@@ -152,3 +152,53 @@ def test_new_tokens_before_a_sequences_start_see_nothing(seqs, split, max_new, d
             assert (np.abs(mine[before:] - want) <= tol).all(), f"sequence {s}"
     t.check_untouched("", "out")
     assert st_lm.st_attn_status(plan) == st_lm.ST_ATTN_BAD_LENGTH
+
+
+def test_rebinding_that_was_captured():
+    """A graph that rebinds does so whenever it is replayed: the plan's own idea of the pointers does not make a later call do nothing."""
+    torch = torch_()
+    tenants = [Tenant(4, 2, 64, "bf16", [(1, 70), (1, 33)], page=16, seed=s).upload() for s in (1, 2)]
+    a, b = tenants
+    plan = st_lm.st_attn_plan([a.desc()], keep=tenants)
+    x, w = torch.randn(2, 3, 64, device="cuda").unbind(0), torch.randn(40, 64, device="cuda")
+    y = [torch.full((3, 40), float("nan"), device="cuda") for _ in range(2)]
+    products = [st_lm.make_matmul_desc(3, 40, 64, "f32", "f32", x[i], w, y[i]) for i in range(2)]
+    product = st_lm.st_matmul_plan([products[0]], keep=[x, w, y])
+    side, graphs = torch.cuda.Stream(), [torch.cuda.CUDAGraph() for _ in range(2)]
+
+    def step(which):
+        st_lm.st_attn_rebind_all(plan, [tenants[which].desc()], side)
+        st_lm.st_attn_run(plan, side)
+        st_lm.st_matmul_rebind_all(product, [products[which]], side)
+        st_lm.st_matmul_run(product, side)
+
+    torch.cuda.synchronize()
+    for which in range(2):         # the first one's pointers are the plan's own already
+        with torch.cuda.graph(graphs[which], stream=side):
+            step(which)
+    want = [(x[i].double() @ w.double().t().contiguous()).cpu() for i in range(2)]
+    tol = [2 * 2.0 ** -24 * 68 * (x[i].double().abs() @ w.double().abs().t().contiguous()).cpu() + 1e-30 for i in range(2)]
+
+    def check(which, what):
+        torch.cuda.synchronize()
+        for i, t in enumerate(tenants):
+            if i == which:
+                t.check_out(what)
+                assert ((y[i].double().cpu() - want[i]).abs() <= tol[i]).all(), what
+            else:
+                assert torch.isnan(t.d["out"]).all() and torch.isnan(y[i]).all(), what
+        for t, z in zip(tenants, y):
+            t.d["out"].fill_(float("nan"))
+            z.fill_(float("nan"))
+        torch.cuda.synchronize()
+
+    step(1)                        # no graph has run yet
+    check(1, "after the captures")
+    for turn in range(3):
+        for eager, replayed in ((0, 1), (1, 0), (0, 0)):
+            step(eager)
+            check(eager, f"eager {eager}, turn {turn}")
+            graphs[replayed].replay()
+            check(replayed, f"replay {replayed}, turn {turn}")
+            step(eager)            # the pointers of the last eager call, but not always those that the replay left
+            check(eager, f"eager {eager} again, turn {turn}")
