@@ -64,11 +64,27 @@ def lib() -> ctypes.CDLL:
 
 
 class _Owned:
-    """Owns a plan handle; keeps the tensors it borrows alive."""
+    """Owns a plan handle and keeps alive what it borrows: every object that was given as `keep`, when the plan was made and at each rebinding, until
+    release() or destroy().  A program that rebinds to new tensors again and again calls release() now and then, or holds its tensors itself."""
     _destroy = ""
 
     def __init__(self, handle: int, keep):
-        self.handle, self._keep = handle, keep
+        self.handle, self._held = handle, {}
+        self._hold(keep)
+
+    def _hold(self, keep):
+        if keep is not None:
+            self._held[id(keep)] = keep
+
+    @property
+    def kept(self) -> list:
+        return list(self._held.values())
+
+    def release(self, keep=None) -> None:
+        """Lets go of all but `keep`, which has to cover what the plan is bound to now.  To be called when the runs that used the rest have ended, and
+        no graph will run them again."""
+        self._held = {}
+        self._hold(keep)
 
     def destroy(self):
         if getattr(self, "handle", None):
@@ -77,6 +93,7 @@ class _Owned:
             except Exception:      # interpreter shutdown
                 pass
             self.handle = None
+            self._held = {}
 
     def __del__(self):
         self.destroy()
@@ -129,8 +146,7 @@ def st_matmul_run(plan: MatmulPlan, stream=None) -> None:
 def st_matmul_rebind_all(plan: MatmulPlan, descs: Sequence[st_matmul_desc], stream=None, keep=None) -> None:
     arr, n = _array(st_matmul_desc, descs)
     _check(lib().st_matmul_rebind_all(plan.handle, arr, n, _stream(stream)), "st_matmul_rebind_all")
-    if keep is not None:
-        plan._keep = (plan._keep, keep)
+    plan._hold(keep)
 
 
 def st_matmul_get_info(plan: MatmulPlan) -> st_matmul_plan_info:
@@ -196,8 +212,7 @@ def st_attn_run(plan: AttnPlan, stream=None) -> None:
 def st_attn_rebind_all(plan: AttnPlan, descs: Sequence[st_attn_desc], stream=None, keep=None) -> None:
     arr, n = _array(st_attn_desc, descs)
     _check(lib().st_attn_rebind_all(plan.handle, arr, n, _stream(stream)), "st_attn_rebind_all")
-    if keep is not None:
-        plan._keep = (plan._keep, keep)
+    plan._hold(keep)
 
 
 def st_attn_status(plan: AttnPlan) -> int:
