@@ -96,7 +96,7 @@ struct AttnDev {
   int32_t least;         // so few that none but the last has fewer than these, and
   int32_t chunk;         // none has more than these.
   float root;            // With kAttnRowsSplit (a step: a tile of the workgroup): one up to `whole` steps, else the square root of root times the
-                         // steps, if that is `most` or more just these, else not more than `want`; but one per kAttnLevelSteps up to `least`
+                         // steps, if that is `most` or more just these, else not more than `want`; but one per attn_level_steps() up to `least`
   uint32_t flip;         // sign bits of two query elements, where scale is negative
   int32_t pad[3];
 };
