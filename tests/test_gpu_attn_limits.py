@@ -202,3 +202,23 @@ def test_rebinding_that_was_captured():
             check(replayed, f"replay {replayed}, turn {turn}")
             step(eager)            # the pointers of the last eager call, but not always those that the replay left
             check(eager, f"eager {eager} again, turn {turn}")
+
+
+@pytest.mark.parametrize("max_new", [None, 4096])
+@pytest.mark.parametrize("dim, dtype", [(64, "bf16"), (64, "f16"), (128, "f16"), (256, "f16"), (256, "bf16")])
+def test_attention_under_every_scale(dim, dtype, max_new):
+    """Sequences of one token, whose value comes out as it is: scales above the largest one that the type writes count as that, the smallest elements are rounded."""
+    torch = torch_()
+    t = Tenant(2, 1, dim, dtype, [(1, 1)] * 255, page=16, filled=False, max_new=max_new)
+    code = np.tile(np.arange(16, dtype=np.uint8), dim // 16)[None]
+    zero, one = np.zeros((1, dim), np.uint8), np.ones((1, dim // 32), np.uint8)
+    for p in range(255):
+        t.pool.write(t.table[p, 0], 0, zero, one, code, p * one)
+    run(t)
+    largest = 141 if dtype == "f16" else 252          # 2^14, 2^125
+    want = decode(code.repeat(255, 0), np.minimum(np.arange(255), largest)[:, None].repeat(dim // 32, 1))
+    most = float(torch.finfo(t.tt).max)
+    want = np.clip(want, -most, most)[:, None].repeat(2, 1)
+    # fp16: multiples of 2^-23, then of 2^-24; bf16: what is below the smallest normal number may be 0
+    off = np.abs(t.outputs()[:255] - want)
+    assert (off <= (np.abs(want) < 2.0 ** -22) * (2.0 ** -24 + 2.0 ** -25) if dtype == "f16" else off <= (np.abs(want) < 2.0 ** -126) * 2.0 ** -126).all()
